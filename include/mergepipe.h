@@ -382,6 +382,156 @@ int mp_lora_merge_ties_tau(const mp_layout* layout, const void* base, const mp_l
                            const uint32_t* mask, const uint32_t* tau, float lambda, void* out,
                            void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Running what a merge made: the feed-forward part of a block
+ *
+ * Products with a checkpoint's weight matrices, its norms, and a layer that
+ * routes a few tokens among the experts' own weights, for evaluating a merged
+ * checkpoint, training on from it, or serving its experts unmerged.  Matrices
+ * are row-major with unit stride inside a row and `ld` elements from one row
+ * to the next (ld >= columns); rows need no alignment beyond an element's, so
+ * tensors are used where a checkpoint holds them.  Rows of whole 16-byte
+ * chunks, starting 16-byte aligned, are fastest.
+ *
+ * Sums are held in fp32 whatever the dtype and each output is rounded once,
+ * to nearest even (exceptions are named where they hold).  Results are the
+ * same bits on every run.  Infinities and NaN propagate as the formulas do.
+ *
+ * These calls take no lock, keep nothing between calls and allocate nothing:
+ * scratch is the caller's `workspace` (device memory, 16-byte aligned, any
+ * content; NULL where the query function says 0 bytes).  Calls on different
+ * streams run together as long as they do not share a workspace, and a call
+ * may be captured in a HIP graph.  All are asynchronous on `stream`.
+ * MP_E_ARG: a null, misaligned, non-device or too small buffer, a size, ld,
+ * flag or code out of range, or an output that overlaps another buffer of
+ * the call (beyond what is allowed below); MP_E_HIP: the launch failed.
+ * Sizes are at most 2^31 - 1 each, ld at most 2^40. */
+typedef enum {
+    MP_ACT_NONE = 0,
+    MP_ACT_RELU = 1,
+    MP_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function */
+    MP_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+    MP_ACT_SILU = 4       /* z / (1 + exp(-z)) */
+} mp_act;
+
+/* A linear layer: x is m x k (tokens x inputs), w is n x k (outputs x
+ * inputs, as checkpoints hold it), y, z and the residual are m x n.  The ld
+ * of a matrix that a call does not have is ignored. */
+typedef struct mp_linear_shape {
+    int32_t dtype; /* mp_dtype of every matrix and vector */
+    int32_t act;   /* mp_act */
+    int64_t m, n, k;
+    int64_t ldx, ldw, ldy, ldz, ldr;
+} mp_linear_shape;
+
+/* y = act(z) + residual, z = x w^T + bias.
+ *   bias: n values, or NULL.  residual: m x n (ldr), or NULL; it may be y
+ *   itself (same pointer and ld).  z: NULL, or m x n (ldz), receives the
+ *   pre-activations, rounded to the dtype, for mp_linear_backward (y is
+ *   formed from the unrounded ones).
+ * k = 0 gives z = bias; m = 0 or n = 0 does nothing.
+ * workspace: mp_linear_workspace(shape, 0, &bytes) bytes. */
+int mp_linear(const mp_linear_shape* shape, const void* x, const void* w, const void* bias,
+              const void* residual, void* y, void* z, void* workspace, uint64_t workspace_bytes,
+              void* stream);
+
+/* Gradients of mp_linear: with dz = dy * act'(z),
+ *   dx = dz w (m x k, lddx), dw = dz^T x (n x k, lddw), dbias[j] = sum over
+ *   the rows of dz; the residual's gradient is dy itself.
+ *   dy: m x n (ldy).  z: m x n (ldz) as stored by mp_linear; may be NULL if
+ *   act is MP_ACT_NONE.  dx, dw, dbias: each may be NULL (not computed); x
+ *   may be NULL without dw, w without dx.  m = 0 gives dw = 0, dbias = 0.
+ * relu's derivative at 0 is 0.  In bf16, with an activation, the products
+ * take dz rounded to bf16 (the type the matrix cores multiply); dbias sums the
+ * unrounded fp32 values.
+ * workspace: mp_linear_workspace(shape, 1, &bytes) bytes. */
+int mp_linear_backward(const mp_linear_shape* shape, const void* dy, const void* x, const void* w,
+                       const void* z, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias,
+                       void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of mp_linear (backward = 0) or mp_linear_backward
+ * (backward = 1, for any choice of its outputs) at this shape.  Host only. */
+int mp_linear_workspace(const mp_linear_shape* shape, int32_t backward, uint64_t* bytes);
+
+/* mp_norm_shape.flags: 0 is layer norm; MP_NORM_RMS takes the mean as 0 (RMS
+ * norm, the norm of the Qwen2.5- and Llama-shaped families). */
+enum { MP_NORM_RMS = 1 };
+
+typedef struct mp_norm_shape {
+    int32_t dtype; /* mp_dtype of x, y, the weight, the bias and their gradients */
+    int32_t flags;
+    int64_t rows, cols;
+    int64_t ldx, ldy;
+    float eps; /* >= 0, finite */
+} mp_norm_shape;
+
+/* y = (x - mean) rstd weight + bias per row, mean = sum x / cols (0 with
+ * MP_NORM_RMS), rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps).
+ *   weight, bias: cols values, or NULL (1 and 0).  mean, rstd: device
+ *   float[rows], or NULL (not stored; mean is not written with MP_NORM_RMS).
+ *   y may be x itself (same pointer and ld). */
+int mp_norm(const mp_norm_shape* shape, const void* x, const void* weight, const void* bias, void* y,
+            float* mean, float* rstd, void* stream);
+
+/* Gradients of mp_norm.  With n = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - average(g) - n average(g n)) (without average(g) for
+ *   MP_NORM_RMS; rows x cols, lddx), dweight = sum over the rows of dy n,
+ *   dbias = sum over the rows of dy.
+ *   dy: rows x cols (ldy).  mean (unused, may be NULL, with MP_NORM_RMS) and
+ *   rstd as mp_norm stored them.  dx, dweight, dbias: each may be NULL (not
+ *   computed); dx may be dy itself (same pointer and ld).  rows = 0 gives
+ *   dweight = dbias = 0.
+ * workspace: mp_norm_workspace(shape, &bytes) bytes. */
+int mp_norm_backward(const mp_norm_shape* shape, const void* dy, const void* x, const void* weight,
+                     const float* mean, const float* rstd, void* dx, int64_t lddx, void* dweight,
+                     void* dbias, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of mp_norm_backward at this shape.  Host only. */
+int mp_norm_workspace(const mp_norm_shape* shape, uint64_t* bytes);
+
+/* A layer that routes tokens among the feed-forward weights of E experts,
+ * read in place: in each expert's buffer (a flat checkpoint), gate and up are
+ * ffn x hidden and down is hidden x ffn, row-major without gaps, at these
+ * element offsets; up_off < 0: no up matrix. */
+enum { MP_MOE_RENORM = 1 };
+typedef struct mp_moe_layer {
+    int32_t dtype; /* mp_dtype of every matrix */
+    int32_t act;   /* mp_act */
+    int32_t top_k; /* experts per token, 1 .. min(E, 8) */
+    int32_t flags; /* 0 or MP_MOE_RENORM */
+    int64_t hidden, ffn;
+    int64_t gate_off, up_off, down_off;
+} mp_moe_layer;
+
+/* Per token: logits l = router x + router_bias; the top_k largest are chosen,
+ * ties to the lowest index, a NaN above every number; expert e's gate is
+ * exp(l_e) / sum of exp(l) over all experts, or, with MP_MOE_RENORM, over the
+ * chosen ones;
+ *   y = residual + sum over the chosen of gate_e down_e h_e,
+ *   h_e = act(gate_e x) * (up_e x)   (act(gate_e x) without up).
+ * A router_bias of -inf shuts an expert out for every token: a chosen expert
+ * whose gate is 0 adds nothing and, if no token has it with another gate, is
+ * not read; a token all of whose logits are -inf gets gates of 0 and y =
+ * residual.
+ *   x: tokens x hidden (ldx), 0 <= tokens <= 64 (MP_E_UNSUPPORTED beyond).
+ *   router: E x hidden.  router_bias: E values of the dtype, or NULL.
+ *   experts: HOST array of E pointers, 1 <= E <= 32; residency MP_DEVICE, or
+ *   MP_HOST_PINNED: pinned host memory, of which only the chosen experts'
+ *   weights cross PCIe.  residual: tokens x hidden (ldr) or NULL; y: tokens x
+ *   hidden (ldy); y may be the residual or x itself (same pointer and ld).
+ *   ids: device int32[tokens * top_k], gates: device float[tokens * top_k],
+ *   the choices in order of decreasing logit, or NULL.
+ * h_e enters the down product as a sum of two values of the dtype (bf16: its
+ * rounding and the rounded remainder), so that it keeps 16 bits.
+ * workspace: mp_moe_workspace(layer, tokens, &bytes) bytes. */
+int mp_moe(const mp_moe_layer* layer, int64_t tokens, const void* x, int64_t ldx, const void* router,
+           const void* router_bias, const void* const* experts, int32_t E, int32_t residency,
+           const void* residual, int64_t ldr, void* y, int64_t ldy, int32_t* ids, float* gates,
+           void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of mp_moe for this many tokens.  Host only. */
+int mp_moe_workspace(const mp_moe_layer* layer, int64_t tokens, uint64_t* bytes);
+
 /* Measurement aid, not part of the method: a plain stream copy of `bytes`
  * bytes (a multiple of 16, at most 2^40) from device memory src to device
  * memory dst, which must not overlap, with the merge kernels' access pattern

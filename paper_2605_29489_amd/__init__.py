@@ -32,11 +32,16 @@ MP_DEVICE, MP_HOST_PINNED, MP_HOST_PAGEABLE, MP_HOST_FILE = 0, 1, 2, 3
 MP_EXPERTS_DELTA = 16  # OR-ed into residency: experts hold W_i - W_0
 MP_COMBINE_LINEAR, MP_COMBINE_SIGN_ELECT = 0, 1
 MP_PLAN_PER_BYTE, MP_PLAN_SKIP_ZERO = 1, 2
+MP_ACT_NONE, MP_ACT_RELU, MP_ACT_GELU, MP_ACT_GELU_TANH, MP_ACT_SILU = range(5)
+MP_NORM_RMS = 1
+MP_MOE_RENORM = 1
 
 EXPORTS = ("mp_layout_blocks", "mp_index_blocks", "mp_index_ties", "mp_ties_tensor_thresholds", "mp_plan",
            "mp_plan_noalloc", "mp_coverage", "mp_merge_avg", "mp_merge_avg_renorm",
            "mp_merge_ties",
            "mp_merge_ties_tau", "mp_merge_dare", "mp_lora_materialize", "mp_lora_merge_ties_tau", "mp_stream_copy",
+           "mp_linear", "mp_linear_backward", "mp_linear_workspace", "mp_norm", "mp_norm_backward",
+           "mp_norm_workspace", "mp_moe", "mp_moe_workspace",
            "mp_set_stage_bytes",
            "mp_set_workspace_limit", "mp_workspace_bytes", "mp_ties_tensor_left", "mp_last_error", "mp_release")
 
@@ -67,6 +72,21 @@ class mp_io_stats(C.Structure):
 class mp_lora_tensor(C.Structure):
     _fields_ = [("tensor", C.c_int32), ("rank", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
                 ("a_off", C.c_int64), ("b_off", C.c_int64), ("scale", C.c_float)]
+
+
+class mp_linear_shape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32)] + [
+        (n, C.c_int64) for n in ("m", "n", "k", "ldx", "ldw", "ldy", "ldz", "ldr")]
+
+
+class mp_norm_shape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ldx", C.c_int64), ("ldy", C.c_int64), ("eps", C.c_float)]
+
+
+class mp_moe_layer(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("top_k", C.c_int32), ("flags", C.c_int32)] + [
+        (n, C.c_int64) for n in ("hidden", "ffn", "gate_off", "up_off", "down_off")]
 
 
 class MPError(RuntimeError):
@@ -108,6 +128,15 @@ def _load():
                                       vp]
     L.mp_lora_merge_ties_tau.argtypes = [lp, vp, C.POINTER(mp_lora_tensor), i32, C.POINTER(vp), i32, vp, vp,
                                          C.c_float, vp, vp]
+    i64, lsp, nsp, mlp = C.c_int64, C.POINTER(mp_linear_shape), C.POINTER(mp_norm_shape), C.POINTER(mp_moe_layer)
+    L.mp_linear.argtypes = [lsp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+    L.mp_linear_backward.argtypes = [lsp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, u64, vp]
+    L.mp_linear_workspace.argtypes = [lsp, i32, C.POINTER(u64)]
+    L.mp_norm.argtypes = [nsp, vp, vp, vp, vp, vp, vp, vp]
+    L.mp_norm_backward.argtypes = [nsp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, u64, vp]
+    L.mp_norm_workspace.argtypes = [nsp, C.POINTER(u64)]
+    L.mp_moe.argtypes = [mlp, i64, vp, i64, vp, vp, C.POINTER(vp), i32, i32, vp, i64, vp, i64, vp, vp, vp, u64, vp]
+    L.mp_moe_workspace.argtypes = [mlp, i64, C.POINTER(u64)]
     L.mp_last_error.restype = C.c_char_p
     L.mp_stream_copy.argtypes = [vp, vp, u64, vp]
     L.mp_set_stage_bytes.argtypes = [u64]
@@ -124,7 +153,9 @@ def _load():
                  "mp_plan_noalloc", "mp_coverage", "mp_merge_avg",
                  "mp_merge_avg_renorm", "mp_merge_ties",
                  "mp_merge_ties_tau",
-                 "mp_merge_dare", "mp_lora_materialize", "mp_lora_merge_ties_tau", "mp_stream_copy"):
+                 "mp_merge_dare", "mp_lora_materialize", "mp_lora_merge_ties_tau", "mp_stream_copy",
+                 "mp_linear", "mp_linear_backward", "mp_linear_workspace", "mp_norm", "mp_norm_backward",
+                 "mp_norm_workspace", "mp_moe", "mp_moe_workspace"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -336,6 +367,217 @@ def mp_lora_merge_ties_tau(layout: Layout, base, loras, adapters, mask, tau, lam
     _check(lib.mp_lora_merge_ties_tau(layout.ref, _ptr(base), recs, len(loras), _ptrs(adapters) if loras else None,
                                       K, _ptr(mask),
                                       _ptr(tau), float(lam), _ptr(out), _stream(stream)))
+
+
+# ------------------------------------------------------------------ the feed-forward part of a block
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return MP_BF16
+    if t.dtype is torch.float32:
+        return MP_F32
+    raise ValueError(f"dtype {t.dtype} is not torch.float32 or torch.bfloat16")
+
+
+def _matrix(t, rows, cols, dtype, name: str) -> int:
+    """Checks a rows x cols matrix of unit column stride; its row stride."""
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    sr, sc = t.stride()
+    if sc != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if rows > 1:
+        if sr < cols:
+            raise ValueError(f"{name}: rows overlap or run backwards (stride {sr})")
+        return sr
+    return max(sr, cols)
+
+
+def _vector(t, n, dtype, name: str):
+    if t is not None:
+        if t.numel() != n or t.dtype is not dtype or not t.is_contiguous():
+            raise ValueError(f"{name}: expected {n} contiguous values of {dtype}")
+
+
+def _scratch(need: int, workspace, like, stream):
+    """(pointer, bytes) of the caller's workspace tensor, or of a new one whose memory torch's allocator
+    keeps for the call's stream; the tensor is returned to be held until the launch."""
+    if need == 0:
+        return None, 0, None
+    import torch
+    if workspace is None:
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        else:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=like.device)
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _linear_shape(dtype, act, m, n, k, ldx=0, ldw=0, ldy=0, ldz=0, ldr=0):
+    return mp_linear_shape(dtype, int(act), m, n, k, ldx, ldw, ldy, ldz, ldr)
+
+
+_WORD = C.c_uint64
+
+
+def _need(fn, *args) -> int:
+    n = _WORD(0)
+    _check(fn(*args, C.byref(n)))
+    return n.value
+
+
+def mp_linear(x, w, y, bias=None, residual=None, act: int = MP_ACT_NONE, z=None, workspace=None, stream=None):
+    """y = act(z) + residual with z = x w^T + bias, into `y` (and `z`, if given).
+
+    ``x``: [m, k]; ``w``: [n, k], as checkpoints hold it; ``y``, ``z``, ``residual``: [m, n]; ``bias``: [n].
+    fp32 or bf16 device tensors, any row stride; ``residual`` may be ``y``.  ``workspace``: a device
+    tensor of ``mp_linear_workspace`` bytes to reuse between calls (default: a new one)."""
+    dt = x.dtype
+    m, k = x.shape
+    n = w.shape[0]
+    s = _linear_shape(_dtype_code(x), act, m, n, k, _matrix(x, m, k, dt, "x"), _matrix(w, n, k, dt, "w"),
+                      _matrix(y, m, n, dt, "y"), 0 if z is None else _matrix(z, m, n, dt, "z"),
+                      0 if residual is None else _matrix(residual, m, n, dt, "residual"))
+    _vector(bias, n, dt, "bias")
+    ref = C.byref(s)
+    wp, wb, hold = _scratch(_need(lib.mp_linear_workspace, ref, 0), workspace, x, stream)
+    _check(lib.mp_linear(ref, x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), _ptr(z), wp, wb,
+                         _stream(stream)))
+
+
+def mp_linear_backward(dy, x=None, w=None, z=None, act: int = MP_ACT_NONE, dx=None, dw=None, dbias=None,
+                       workspace=None, stream=None):
+    """Gradients of ``mp_linear`` into those of ``dx`` [m, k], ``dw`` [n, k] and ``dbias`` [n] that are given.
+
+    ``dy``: [m, n]; ``z``: the pre-activations that mp_linear stored (needed with an activation); ``x`` is
+    needed for dw, ``w`` for dx.  The residual's gradient is dy."""
+    dt = dy.dtype
+    m, n = dy.shape
+    if (dx is None) != (dx is None or w is None) or (dw is None) != (dw is None or x is None):
+        raise ValueError("dx needs w, and dw needs x")
+    k = dx.shape[1] if dx is not None else dw.shape[1] if dw is not None else 0
+    if act != MP_ACT_NONE and z is None:
+        raise ValueError("an activation needs z")
+    s = _linear_shape(_dtype_code(dy), act, m, n, k, 0 if dw is None else _matrix(x, m, k, dt, "x"),
+                      0 if dx is None else _matrix(w, n, k, dt, "w"), _matrix(dy, m, n, dt, "dy"),
+                      0 if act == MP_ACT_NONE else _matrix(z, m, n, dt, "z"))
+    lddx = 0 if dx is None else _matrix(dx, m, k, dt, "dx")
+    lddw = 0 if dw is None else _matrix(dw, n, k, dt, "dw")
+    _vector(dbias, n, dt, "dbias")
+    ref = C.byref(s)
+    wp, wb, hold = _scratch(_need(lib.mp_linear_workspace, ref, 1), workspace, dy, stream)
+    _check(lib.mp_linear_backward(ref, dy.data_ptr(), _ptr(x) if dw is not None else None,
+                                  _ptr(w) if dx is not None else None, _ptr(z) if act != MP_ACT_NONE else None,
+                                  _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), wp, wb, _stream(stream)))
+
+
+def mp_linear_workspace(dtype: int, act: int, m: int, n: int, k: int, backward: bool = False) -> int:
+    s = _linear_shape(dtype, act, m, n, k)
+    return _need(lib.mp_linear_workspace, C.byref(s), int(backward))
+
+
+def mp_norm(x, y, weight=None, bias=None, eps: float = 1e-6, rms: bool = False, mean=None, rstd=None, stream=None):
+    """Layer norm (``rms``: RMS norm) of the rows of ``x`` [rows, cols] into ``y``, which may be ``x``;
+    per-row statistics into the fp32 ``mean`` and ``rstd`` [rows], if given."""
+    dt = x.dtype
+    rows, cols = x.shape
+    s = mp_norm_shape(_dtype_code(x), MP_NORM_RMS if rms else 0, rows, cols, _matrix(x, rows, cols, dt, "x"),
+                      _matrix(y, rows, cols, dt, "y"), eps)
+    _vector(weight, cols, dt, "weight")
+    _vector(bias, cols, dt, "bias")
+    _stats(rows, mean, rstd)
+    _check(lib.mp_norm(C.byref(s), x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), _ptr(mean), _ptr(rstd),
+                       _stream(stream)))
+
+
+def _stats(rows, *ts):
+    import torch
+    for t in ts:
+        _vector(t, rows, torch.float32, "mean or rstd")
+
+
+def mp_norm_backward(dy, x, rstd, mean=None, weight=None, rms: bool = False, dx=None, dweight=None, dbias=None,
+                     workspace=None, stream=None):
+    """Gradients of ``mp_norm`` into those of ``dx`` [rows, cols] (which may be ``dy``), ``dweight`` and
+    ``dbias`` [cols] that are given, from the statistics that mp_norm stored."""
+    dt = x.dtype
+    rows, cols = x.shape
+    s = mp_norm_shape(_dtype_code(x), MP_NORM_RMS if rms else 0, rows, cols, _matrix(x, rows, cols, dt, "x"),
+                      _matrix(dy, rows, cols, dt, "dy"), 0.0)
+    lddx = 0 if dx is None else _matrix(dx, rows, cols, dt, "dx")
+    _vector(weight, cols, dt, "weight")
+    _vector(dweight, cols, dt, "dweight")
+    _vector(dbias, cols, dt, "dbias")
+    _stats(rows, mean, rstd)
+    if mean is None and not rms:
+        raise ValueError("layer norm needs mean")
+    ref = C.byref(s)
+    wp, wb, hold = _scratch(_need(lib.mp_norm_workspace, ref), workspace, x, stream)
+    _check(lib.mp_norm_backward(ref, dy.data_ptr(), x.data_ptr(), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), lddx,
+                                _ptr(dweight), _ptr(dbias), wp, wb, _stream(stream)))
+
+
+def mp_norm_workspace(dtype: int, rows: int, cols: int, rms: bool = False) -> int:
+    s = mp_norm_shape(dtype, MP_NORM_RMS if rms else 0, rows, cols, cols, cols, 0.0)
+    return _need(lib.mp_norm_workspace, C.byref(s))
+
+
+@dataclass
+class MoeLayer:
+    """mp_moe_layer: where an expert's checkpoint holds its feed-forward matrices (element offsets; gate and
+    up are ffn x hidden, down is hidden x ffn; up_off None: no up matrix), and how tokens are routed."""
+
+    hidden: int
+    ffn: int
+    top_k: int
+    gate_off: int
+    up_off: Optional[int]
+    down_off: int
+    act: int = MP_ACT_SILU
+    renorm: bool = False
+
+    def _struct(self, dtype: int):
+        return mp_moe_layer(dtype, int(self.act), self.top_k, MP_MOE_RENORM if self.renorm else 0, self.hidden,
+                            self.ffn, self.gate_off, -1 if self.up_off is None else self.up_off, self.down_off)
+
+
+def mp_moe(layer: MoeLayer, x, router, experts, y, ids=None, gates=None, router_bias=None, residual=None,
+           residency: int = MP_DEVICE, workspace=None, stream=None):
+    """A mixture-of-experts layer for a few tokens: ``x`` [tokens, hidden] through the ``top_k`` experts that
+    ``router`` [E, hidden] chooses, into ``y``; the choices into ``ids`` (int32) and ``gates`` (fp32)
+    [tokens, top_k], if given.  ``experts``: E flat checkpoints (residency MP_DEVICE or MP_HOST_PINNED)."""
+    import torch
+    dt = x.dtype
+    T, D = x.shape
+    E = len(experts)
+    s = layer._struct(_dtype_code(x))
+    ldx, ldy = _matrix(x, T, layer.hidden, dt, "x"), _matrix(y, T, D, dt, "y")
+    ldr = 0 if residual is None else _matrix(residual, T, D, dt, "residual")
+    if router.shape != (E, D) or router.dtype is not dt or not router.is_contiguous():
+        raise ValueError(f"router: expected a contiguous {(E, D)} matrix of {dt}")
+    _vector(router_bias, E, dt, "router_bias")
+    _vector(ids, T * layer.top_k, torch.int32, "ids")
+    _vector(gates, T * layer.top_k, torch.float32, "gates")
+    need = max(layer.gate_off, layer.down_off, layer.up_off or 0) + layer.hidden * layer.ffn
+    for e in experts:
+        if e.dtype is not dt or e.numel() < need or not e.is_contiguous():
+            raise ValueError(f"experts: expected flat checkpoints of at least {need} values of {dt}")
+    ref = C.byref(s)
+    wp, wb, hold = _scratch(_need(lib.mp_moe_workspace, ref, T), workspace, x, stream)
+    _check(lib.mp_moe(ref, T, x.data_ptr(), ldx, router.data_ptr(), _ptr(router_bias), _ptrs(experts), E, residency,
+                      _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(ids), _ptr(gates), wp, wb, _stream(stream)))
+
+
+def mp_moe_workspace(layer: MoeLayer, dtype: int, tokens: int) -> int:
+    s = layer._struct(dtype)
+    return _need(lib.mp_moe_workspace, C.byref(s), tokens)
 
 
 def mp_last_error() -> str:

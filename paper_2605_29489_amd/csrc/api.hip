@@ -32,6 +32,8 @@ namespace {
 
 thread_local std::string g_err;
 
+}  // namespace
+
 int fail(int code, const char* fmt, ...)
 {
     char buf[512];
@@ -48,6 +50,10 @@ int hip_fail(hipError_t e, const char* what)
     // an allocation that failed (or passed the workspace limit) is MP_E_NOMEM
     return fail(e == hipErrorOutOfMemory ? MP_E_NOMEM : MP_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+void clear_error() { g_err.clear(); }
+
+namespace {
 
 // ------------------------------------------------------------ workspaces
 uint64_t g_ws_limit = 0;  // bytes; 0 = no limit
@@ -353,6 +359,8 @@ struct Range {
     const char* name;
 };
 
+}  // namespace
+
 int check_device_buffer(const void* p, size_t bytes, const char* name)
 {
     if (p == nullptr)
@@ -423,6 +431,8 @@ int check_pinned_buffer(const void* p, size_t bytes, const char* name, const voi
         (void)hipGetLastError();  // unified addressing: the host address is the device address
     return MP_OK;
 }
+
+namespace {
 
 // Host memory of any kind (pageable or pinned) for MP_HOST_PAGEABLE: the
 // library reads it on the host only.  Device memory is refused; the size of

@@ -254,6 +254,55 @@ hipError_t launch_merge_staged(const BlockTable& bt, const MergeArgs& a, const v
 // memory (k_copy.hip).
 hipError_t launch_stream_copy(const void* src, void* dst, uint64_t nbytes, hipStream_t s);
 
+// ---------------------------------------------------------------- the feed-forward part (api_ffn.hip)
+// Arguments below are validated: sizes positive unless stated otherwise.
+
+// y = act(x w^T + bias) + residual (k_linear.hip); bias, residual and z may be null.
+hipError_t launch_linear(const mp_linear_shape& s, const void* x, const void* w, const void* bias,
+                         const void* residual, void* y, void* z, void* ws, hipStream_t st);
+uint64_t linear_ws_bytes(const mp_linear_shape& s);
+// dx, dw and dbias of it (each may be null).  m may be 0.
+hipError_t launch_linear_backward(const mp_linear_shape& s, const void* dy, const void* x, const void* w,
+                                  const void* z, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias,
+                                  void* ws, hipStream_t st);
+uint64_t linear_backward_ws_bytes(const mp_linear_shape& s);
+
+// Layer or RMS norm and its gradients (k_norm.hip).
+hipError_t launch_norm(const mp_norm_shape& s, const void* x, const void* weight, const void* bias, void* y,
+                       float* mean, float* rstd, hipStream_t st);
+// rows may be 0.
+hipError_t launch_norm_backward(const mp_norm_shape& s, const void* dy, const void* x, const void* weight,
+                                const float* mean, const float* rstd, void* dx, int64_t lddx, void* dweight,
+                                void* dbias, void* ws, hipStream_t st);
+uint64_t norm_ws_bytes(const mp_norm_shape& s);
+
+// A few tokens through E experts (k_moe.hip).
+constexpr int kMoeMaxTokens = 64, kMoeMaxTop = 8;
+struct MoeArgs {
+    mp_moe_layer l;
+    int T, E;
+    const void* x;
+    int64_t ldx;
+    const void* router;
+    const void* router_bias;  // or null
+    const void* residual;     // or null
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    int32_t* ids;  // or null
+    float* gates;  // or null
+};
+hipError_t launch_moe(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStream_t st);
+uint64_t moe_ws_bytes(const mp_moe_layer& l, int64_t tokens);
+
+// ---------------------------------------------------------------- host helpers (api.hip)
+int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+int hip_fail(hipError_t e, const char* what);
+void clear_error();
+// Device memory of at least `bytes` bytes from p on the current device.
+int check_device_buffer(const void* p, size_t bytes, const char* name);
+int check_pinned_buffer(const void* p, size_t bytes, const char* name, const void** dev);
+
 // z with P(|Z| > z) = rho for a standard normal Z (0 unless 0 < rho < 1);
 // scales the TIES kernels' first guess at a trim threshold (k_index.hip).
 double normal_two_sided_quantile(double rho);
