@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "../../include/mergepipe.h"
+#include "device_common.h"
 
 namespace mp {
 
@@ -21,6 +22,60 @@ template <>
 struct Elem<MP_BF16> {
     using T = __bf16;
 };
+
+// ---------------------------------------------------------------- 16-byte access at element alignment
+// Global memory takes 16-byte accesses at any element's alignment, so a row
+// that starts off a 16-byte boundary costs no other code, only lines that two
+// accesses share.
+typedef u32x4_t u32x4_a2 __attribute__((aligned(2)));
+__device__ inline uint4 ld16u(const void* p)
+{
+    const u32x4_t v = *static_cast<const u32x4_a2*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ inline void st16u(void* p, uint4 c)
+{
+    const u32x4_t v = {c.x, c.y, c.z, c.w};
+    *static_cast<u32x4_a2*>(p) = v;
+}
+// The first n (0 <= n < the chunk's elements) elements at p, zeros after them.
+template <int DT>
+__device__ inline uint4 ld16_head(const void* p, int64_t n)
+{
+    uint32_t w[4] = {0, 0, 0, 0};
+    if constexpr (DT == MP_F32) {
+        const uint32_t* q = static_cast<const uint32_t*>(p);
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (j < n)
+                w[j] = q[j];
+    } else {
+        const uint16_t* q = static_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n)
+                w[j / 2] |= (uint32_t)q[j] << (16 * (j & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int DT>
+__device__ inline void st16_head(void* p, uint4 c, int64_t n)
+{
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    if constexpr (DT == MP_F32) {
+        uint32_t* q = static_cast<uint32_t*>(p);
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (j < n)
+                q[j] = w[j];
+    } else {
+        uint16_t* q = static_cast<uint16_t*>(p);
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n)
+                q[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+    }
+}
 
 // ---------------------------------------------------------------- activations
 // In fp32, from exp and erf only.  1 / (1 + exp(-u)) is taken with the
@@ -88,14 +143,6 @@ __device__ inline float act_slope_of(int act, float z)
         case MP_ACT_SILU: return act_slope_f<MP_ACT_SILU>(z);
         default: return 1.0f;
     }
-}
-
-// Sum over the wave, the same bits in every lane.
-__device__ inline float wave_sum(float v)
-{
-    for (int o = 32; o > 0; o >>= 1)
-        v += __shfl_xor(v, o, 64);
-    return v;
 }
 
 }  // namespace mp

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void k_route(MoeArgs a, int32_t* ids, float* g
         float s = 0.0f;
         for (int64_t d = lane; d < a.l.hidden; d += 64)
             s = fmaf((float)x[d], (float)r[d], s);
-        s = wave_sum(s);
+        s = wave_xor_sum(s);
         if (lane == 0)
             lg[e] = a.router_bias ? s + (float)static_cast<const T*>(a.router_bias)[e] : s;
     }
@@ -75,9 +75,9 @@ __global__ __launch_bounds__(256) void k_up(MoeArgs a, ExpertPtrs ex, const int3
         if (a.l.up_off >= 0)
             u = fmaf((float)x[d], (float)w[a.l.up_off + f * D + d], u);
     }
-    g = act_of(a.l.act, wave_sum(g));
+    g = act_of(a.l.act, wave_xor_sum(g));
     if (a.l.up_off >= 0)
-        g *= wave_sum(u);
+        g *= wave_xor_sum(u);
     if (lane == 0)
         h[(int64_t)slot * a.l.ffn + f] = g;
 }
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(256) void k_down(MoeArgs a, ExpertPtrs ex, const in
         float s = 0.0f;
         for (int64_t f = lane; f < F; f += 64)
             s = fmaf((float)w[f], h[(int64_t)slot * F + f], s);
-        y = fmaf(g, wave_sum(s), y);
+        y = fmaf(g, wave_xor_sum(s), y);
     }
     if (lane == 0) {
         if (a.residual)
