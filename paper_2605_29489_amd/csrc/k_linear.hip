@@ -1,5 +1,6 @@
 // A linear layer with bias, activation and residual, and its backward pass.
 #include "ffn_common.h"
+#include "mm_few.h"
 #include "mp_internal.h"
 
 namespace mp {
@@ -54,6 +55,101 @@ __global__ __launch_bounds__(256) void k_gemm(const T* a, int64_t ai, int64_t ap
                 y += (float)static_cast<const T*>(e.r)[i * e.ldr + j];
             c[i * ldc + j] = (T)y;
         }
+}
+
+// ---------------------------------------------------------------- a few tokens
+// A workgroup takes NA tiles of 16 weight rows, its W waves split k, and the
+// partial tiles meet in LDS.
+template <int DT, int NA, int TT, int W>
+__global__ __launch_bounds__(64 * W) void k_linear_few(const char* x, int64_t ldx, const char* w, int64_t ldw,
+                                                       typename Elem<DT>::T* y, int64_t ldy, int M, int64_t N,
+                                                       int64_t K, Epi e)
+{
+    using T = typename Elem<DT>::T;
+    constexpr int es = Fmt<DT>::esize;
+    __shared__ float4 red[W * NA * TT * 64];
+    const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * NA), whole = few_whole<DT>(K);
+    const char *wp[NA], *xp[TT];
+    bool go[TT];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {  // rows past the last repeat it; their outputs are dropped
+        const int64_t r = n0 + i * 16 + (lane & 15);
+        wp[i] = w + (r < N ? r : N - 1) * ldw * es + (lane >> 4) * 16;
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const int r = t * 16 + (lane & 15);
+        go[t] = r < M;
+        xp[t] = go[t] ? x + (int64_t)r * ldx * es + (lane >> 4) * 16 : reinterpret_cast<const char*>(g_zero_steps);
+    }
+    f32x4 acc[NA][TT] = {};
+    few_steps<DT, NA, TT, 1, few_unroll(NA + TT)>(acc, wp, xp, go, whole * wave / W, whole * (wave + 1) / W);
+    if (wave == W - 1 && few_rest<DT>(K))
+        few_tail<DT, NA, TT, 1>(acc, wp, xp, go, whole, few_rest<DT>(K));
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+            red[((wave * NA + i) * TT + t) * 64 + lane] =
+                make_float4(acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]);
+    __syncthreads();
+    sum_tiles<NA * TT>(red, W, threadIdx.x, 64 * W, [&](int q, const float4& s) {
+        const int t = (q >> 6) % TT * 16 + (q & 15);
+        const int64_t j0 = n0 + (q >> 6) / TT * 16 + ((q & 63) >> 4) * 4;
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        if (t >= M)
+            return;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t j = j0 + u;
+            if (j >= N)
+                break;
+            float z = v[u];
+            if (e.bias)
+                z += (float)static_cast<const T*>(e.bias)[j];
+            if (e.z)
+                static_cast<T*>(e.z)[t * e.ldz + j] = (T)z;
+            float a = act_of(e.act, z);
+            if (e.r)
+                a += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
+            y[t * ldy + j] = (T)a;
+        }
+    });
+}
+
+constexpr int kFewTokens = 64;
+
+template <int DT, int NA, int TT>
+hipError_t few_go(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
+{
+    // waves to fill the chip, with 8 steps each at least
+    const int64_t tiles = (s.n + 16 * NA - 1) / (16 * NA), whole = few_whole<DT>(s.k);
+    const int64_t most = whole / 8, want = 4096 / tiles;
+    const int64_t W = want < most ? want : most;
+    const dim3 g((unsigned)tiles);
+    using T = typename Elem<DT>::T;
+#define MP_FEW(w_)                                                                                              \
+    hipLaunchKernelGGL((k_linear_few<DT, NA, TT, w_>), g, dim3(64 * w_), 0, st, (const char*)x, s.ldx,            \
+                       (const char*)w, s.ldw, (T*)y, s.ldy, (int)s.m, s.n, s.k, e)
+    if (W >= 16)
+        MP_FEW(16);
+    else if (W >= 8)
+        MP_FEW(8);
+    else
+        MP_FEW(4);
+#undef MP_FEW
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
+{
+    if (s.m <= 16)
+        return few_go<DT, 1, 1>(s, x, w, y, e, st);
+    if (s.m <= 32)
+        return few_go<DT, 2, 2>(s, x, w, y, e, st);
+    return few_go<DT, 2, 4>(s, x, w, y, e, st);
 }
 
 template <typename T>
@@ -115,6 +211,8 @@ hipError_t launch_linear(const mp_linear_shape& s, const void* x, const void* w,
                          const void* residual, void* y, void* z, void* ws, hipStream_t st)
 {
     const Epi e{bias, residual, z, s.ldr, s.ldz, s.act};
+    if (s.m <= kFewTokens)
+        return s.dtype == MP_F32 ? linear_few<MP_F32>(s, x, w, y, e, st) : linear_few<MP_BF16>(s, x, w, y, e, st);
     return s.dtype == MP_F32 ? gemm<float>(x, s.ldx, 1, w, s.ldw, 1, y, s.ldy, s.m, s.n, s.k, e, st)
                              : gemm<__bf16>(x, s.ldx, 1, w, s.ldw, 1, y, s.ldy, s.m, s.n, s.k, e, st);
 }
