@@ -1,61 +1,11 @@
 // A linear layer with bias, activation and residual, and its backward pass.
 #include "ffn_common.h"
+#include "gemm.h"
 #include "mm_few.h"
 #include "mp_internal.h"
 
 namespace mp {
 namespace {
-
-struct Epi {
-    const void* bias;
-    const void* r;
-    void* z;
-    int64_t ldr, ldz;
-    int act;
-};
-
-// C[i][j] = epilogue(sum over p of A(i, p) B(j, p)), A(i, p) = a[i * ai + p * ap], B(j, p) = b[j * bj + p * bp]:
-// a 64 x 64 tile per workgroup, 4 x 4 outputs per thread, 16 steps of p through LDS at a time.
-template <typename T>
-__global__ __launch_bounds__(256) void k_gemm(const T* a, int64_t ai, int64_t ap, const T* b, int64_t bj, int64_t bp,
-                                              T* c, int64_t ldc, int64_t I, int64_t J, int64_t P, Epi e)
-{
-    __shared__ float sa[16][65], sb[16][65];
-    const int64_t i0 = (int64_t)blockIdx.y * 64, j0 = (int64_t)blockIdx.x * 64;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int64_t p0 = 0; p0 < P; p0 += 16) {
-        __syncthreads();
-        for (int q = threadIdx.x; q < 1024; q += 256) {
-            const int l = ap == 1 ? q >> 4 : q & 63, p = ap == 1 ? q & 15 : q >> 6;
-            sa[p][l] = i0 + l < I && p0 + p < P ? (float)a[(i0 + l) * ai + (p0 + p) * ap] : 0.0f;
-        }
-        for (int q = threadIdx.x; q < 1024; q += 256) {
-            const int l = bp == 1 ? q >> 4 : q & 63, p = bp == 1 ? q & 15 : q >> 6;
-            sb[p][l] = j0 + l < J && p0 + p < P ? (float)b[(j0 + l) * bj + (p0 + p) * bp] : 0.0f;
-        }
-        __syncthreads();
-        for (int p = 0; p < 16; ++p)
-            for (int u = 0; u < 4; ++u)
-                for (int v = 0; v < 4; ++v)
-                    acc[u][v] = fmaf(sa[p][ty + 16 * u], sb[p][tx + 16 * v], acc[u][v]);
-    }
-    for (int u = 0; u < 4; ++u)
-        for (int v = 0; v < 4; ++v) {
-            const int64_t i = i0 + ty + 16 * u, j = j0 + tx + 16 * v;
-            if (i >= I || j >= J)
-                continue;
-            float z = acc[u][v];
-            if (e.bias)
-                z += (float)static_cast<const T*>(e.bias)[j];
-            if (e.z)
-                static_cast<T*>(e.z)[i * e.ldz + j] = (T)z;
-            float y = act_of(e.act, z);
-            if (e.r)
-                y += (float)static_cast<const T*>(e.r)[i * e.ldr + j];
-            c[i * ldc + j] = (T)y;
-        }
-}
 
 // ---------------------------------------------------------------- a few tokens
 // A workgroup takes NA tiles of 16 weight rows, its W waves split k, and the
@@ -152,57 +102,124 @@ hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, vo
     return few_go<DT, 2, 4>(s, x, w, y, e, st);
 }
 
-template <typename T>
-hipError_t gemm(const void* a, int64_t ai, int64_t ap, const void* b, int64_t bj, int64_t bp, void* c, int64_t ldc,
-                int64_t I, int64_t J, int64_t P, const Epi& e, hipStream_t st)
+// ---------------------------------------------------------------- dz
+// dz = dy * act'(z) in the dtype, and the columns' sums of the unrounded
+// values: a workgroup takes 512 (bf16) or 256 (fp32) columns of every
+// gridDim.y-th band of 4 rows, a chunk per thread, and writes one partial row.
+template <int DT, int ACT>
+__global__ __launch_bounds__(256) void k_dz(const typename Elem<DT>::T* dy, int64_t lddy,
+                                            const typename Elem<DT>::T* z, int64_t ldz, typename Elem<DT>::T* dz,
+                                            int64_t lddz, float* part, int64_t pitch, int64_t M, int64_t N)
 {
-    const dim3 g((unsigned)((J + 63) / 64), (unsigned)((I + 63) / 64));
-    hipLaunchKernelGGL(k_gemm<T>, g, dim3(256), 0, st, (const T*)a, ai, ap, (const T*)b, bj, bp, (T*)c, ldc, I, J, P,
-                       e);
-    return hipGetLastError();
-}
-
-// dz = dy * act'(z), and its column sums: one thread per column.
-template <typename T>
-__global__ __launch_bounds__(256) void k_dz(const T* dy, int64_t lddy, const T* z, int64_t ldz, int act, T* dz, T* db,
-                                            int64_t M, int64_t N)
-{
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j >= N)
-        return;
-    float s = 0.0f;
-    for (int64_t i = 0; i < M; ++i) {
-        float v = (float)dy[i * lddy + j];
-        if (act != MP_ACT_NONE)
-            v *= act_slope_of(act, (float)z[i * ldz + j]);
-        s += v;
-        if (dz)
-            dz[i * N + j] = (T)v;
+    constexpr int V = Fmt<DT>::V;
+    __shared__ float4 red[3][V / 4][64];
+    const int lane = threadIdx.x & 63, band = threadIdx.x >> 6;
+    const int64_t j = ((int64_t)blockIdx.x * 64 + lane) * V, have = N - j;
+    float s[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+        s[u] = 0.0f;
+    auto get = [&](const typename Elem<DT>::T* p) {
+        return have >= V ? ld16u(p) : have > 0 ? ld16_head<DT>(p, have) : make_uint4(0, 0, 0, 0);
+    };
+    const int64_t step = (int64_t)gridDim.y * 4;
+    for (int64_t i = (int64_t)blockIdx.y * 4 + band; i < M; i += step) {
+        float d[V];
+        const uint4 dc = get(dy + i * lddy + j);
+        if constexpr (ACT != MP_ACT_NONE) {
+            float f[V];
+            const uint4 zc = get(z + i * ldz + j);
+            Fmt<DT>::unpack(dc, d);
+            Fmt<DT>::unpack(zc, f);
+#pragma unroll
+            for (int u = 0; u < V; ++u)
+                d[u] *= act_slope_f<ACT>(f[u]);
+            if (dz) {  // rows of whole chunks; the columns past N are not read
+                if (have > 0)
+                    st16u(dz + i * lddz + j, Fmt<DT>::pack(d));
+            }
+        } else {
+            Fmt<DT>::unpack(dc, d);
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            s[u] += d[u];
     }
-    if (db)
-        db[j] = (T)s;
+    if (!part)
+        return;
+    if (band > 0)
+#pragma unroll
+        for (int u = 0; u < V / 4; ++u)
+            red[band - 1][u][lane] = make_float4(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
+    __syncthreads();
+    if (band == 0 && have > 0) {
+#pragma unroll
+        for (int u = 0; u < V / 4; ++u) {
+            float4 v = make_float4(s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const float4 r = red[k][u][lane];
+                v.x += r.x;
+                v.y += r.y;
+                v.z += r.z;
+                v.w += r.w;
+            }
+            *reinterpret_cast<float4*>(part + blockIdx.y * pitch + j + 4 * u) = v;
+        }
+    }
 }
 
-template <typename T>
-hipError_t back_t(const mp_linear_shape& s, const void* dy, const void* x, const void* w, const void* z, void* dx,
-                  int64_t lddx, void* dw, int64_t lddw, void* db, void* ws, hipStream_t st)
+// Bands of k_dz: enough workgroups to fill the chip, 8 rows a thread at least.
+int dz_bands(const mp_linear_shape& s)
 {
-    const bool act = s.act != MP_ACT_NONE;
-    hipError_t e = hipSuccess;
-    if (s.n > 0 && (act || db))
-        hipLaunchKernelGGL(k_dz<T>, dim3((unsigned)((s.n + 255) / 256)), dim3(256), 0, st, (const T*)dy, s.ldy,
-                           (const T*)z, s.ldz, s.act, act ? (T*)ws : nullptr, (T*)db, s.m, s.n);
-    if ((e = hipGetLastError()) != hipSuccess)
-        return e;
-    const void* dz = act ? ws : dy;
-    const int64_t lddz = act ? s.n : s.ldy;
-    const Epi none{};
-    if (dx && s.m > 0 && s.k > 0 &&
-        (e = gemm<T>(dz, lddz, 1, w, 1, s.ldw, dx, lddx, s.m, s.k, s.n, none, st)) != hipSuccess)
-        return e;
-    if (dw && s.n > 0 && s.k > 0)
-        e = gemm<T>(dz, 1, lddz, x, 1, s.ldx, dw, lddw, s.n, s.k, s.m, none, st);
-    return e;
+    const int V = s.dtype == MP_F32 ? 4 : 8;
+    const int64_t across = (s.n + 64 * V - 1) / (64 * V), want = (2048 + across - 1) / across, most = (s.m + 31) / 32;
+    const int64_t n = want < most ? want : most;
+    return (int)(n < 1 ? 1 : n > 512 ? 512 : n);
+}
+
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// The workspace of a backward pass: dz, the partial rows of dbias, and what the products need, one after the other.
+struct BackWs {
+    uint64_t dz, part, gemm, bytes;
+    int64_t lddz;
+};
+BackWs back_ws(const mp_linear_shape& s)
+{
+    BackWs w{};
+    const uint64_t es = s.dtype == MP_F32 ? 4 : 2;
+    w.lddz = up(s.n, 8);
+    w.part = s.act != MP_ACT_NONE ? up((int64_t)((uint64_t)s.m * (uint64_t)w.lddz * es), 16) : 0;
+    w.gemm = w.part + (uint64_t)dz_bands(s) * (uint64_t)w.lddz * 4;
+    uint64_t g = 0;
+    if (s.m > 0 && s.n > 0 && s.k > 0) {
+        const uint64_t a = gemm_ws_bytes(s.dtype, Form::NN, s.m, s.k, s.n);
+        const uint64_t b = gemm_ws_bytes(s.dtype, Form::TN, s.n, s.k, s.m);
+        g = a > b ? a : b;
+    }
+    w.bytes = w.gemm + g;
+    return w;
+}
+
+template <int DT>
+hipError_t dz_go(const mp_linear_shape& s, const void* dy, const void* z, void* dz, float* part, const BackWs& w,
+                 hipStream_t st)
+{
+    using T = typename Elem<DT>::T;
+    const dim3 g((unsigned)((s.n + 64 * Fmt<DT>::V - 1) / (64 * Fmt<DT>::V)), dz_bands(s));
+    auto go = [&](auto act) {
+        hipLaunchKernelGGL((k_dz<DT, decltype(act)::value>), g, dim3(256), 0, st, (const T*)dy, s.ldy, (const T*)z,
+                           s.ldz, (T*)dz, w.lddz, part, w.lddz, s.m, s.n);
+    };
+    switch (s.act) {
+        case MP_ACT_RELU: go(std::integral_constant<int, MP_ACT_RELU>{}); break;
+        case MP_ACT_GELU: go(std::integral_constant<int, MP_ACT_GELU>{}); break;
+        case MP_ACT_GELU_TANH: go(std::integral_constant<int, MP_ACT_GELU_TANH>{}); break;
+        case MP_ACT_SILU: go(std::integral_constant<int, MP_ACT_SILU>{}); break;
+        default: go(std::integral_constant<int, MP_ACT_NONE>{}); break;
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -213,25 +230,48 @@ hipError_t launch_linear(const mp_linear_shape& s, const void* x, const void* w,
     const Epi e{bias, residual, z, s.ldr, s.ldz, s.act};
     if (s.m <= kFewTokens)
         return s.dtype == MP_F32 ? linear_few<MP_F32>(s, x, w, y, e, st) : linear_few<MP_BF16>(s, x, w, y, e, st);
-    return s.dtype == MP_F32 ? gemm<float>(x, s.ldx, 1, w, s.ldw, 1, y, s.ldy, s.m, s.n, s.k, e, st)
-                             : gemm<__bf16>(x, s.ldx, 1, w, s.ldw, 1, y, s.ldy, s.m, s.n, s.k, e, st);
+    const Gemm g{s.dtype, Form::NT, x, w, y, s.ldx, s.ldw, s.ldy, s.m, s.n, s.k, e};
+    return launch_gemm(g, ws, st);
 }
 
-uint64_t linear_ws_bytes(const mp_linear_shape& s) { return 0; }
+uint64_t linear_ws_bytes(const mp_linear_shape& s)
+{
+    if (s.m <= kFewTokens || s.n == 0)
+        return 0;
+    return gemm_ws_bytes(s.dtype, Form::NT, s.m, s.n, s.k);
+}
 
 hipError_t launch_linear_backward(const mp_linear_shape& s, const void* dy, const void* x, const void* w,
                                   const void* z, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias,
                                   void* ws, hipStream_t st)
 {
-    return s.dtype == MP_F32 ? back_t<float>(s, dy, x, w, z, dx, lddx, dw, lddw, dbias, ws, st)
-                             : back_t<__bf16>(s, dy, x, w, z, dx, lddx, dw, lddw, dbias, ws, st);
+    const bool act = s.act != MP_ACT_NONE;
+    const BackWs l = back_ws(s);
+    char* base = static_cast<char*>(ws);
+    hipError_t e = hipSuccess;
+    if (s.n > 0 && ((act && (dx || dw)) || dbias)) {
+        float* part = dbias ? reinterpret_cast<float*>(base + l.part) : nullptr;
+        void* to = act && (dx || dw) ? base + l.dz : nullptr;
+        e = s.dtype == MP_F32 ? dz_go<MP_F32>(s, dy, z, to, part, l, st) : dz_go<MP_BF16>(s, dy, z, to, part, l, st);
+        if (e == hipSuccess && dbias)
+            e = launch_sum_rows(s.dtype, part, dz_bands(s), l.lddz, s.n, dbias, st);
+        if (e != hipSuccess)
+            return e;
+    }
+    const void* dz = act ? static_cast<const void*>(base + l.dz) : dy;
+    const int64_t lddz = act ? l.lddz : s.ldy;
+    if (dx && s.m > 0 && s.k > 0) {
+        const Gemm g{s.dtype, Form::NN, dz, w, dx, lddz, s.ldw, lddx, s.m, s.k, s.n, Epi{}};
+        if ((e = launch_gemm(g, base + l.gemm, st)) != hipSuccess)
+            return e;
+    }
+    if (dw && s.n > 0 && s.k > 0) {
+        const Gemm g{s.dtype, Form::TN, dz, x, dw, lddz, s.ldx, lddw, s.n, s.k, s.m, Epi{}};
+        e = launch_gemm(g, base + l.gemm, st);
+    }
+    return e;
 }
 
-uint64_t linear_backward_ws_bytes(const mp_linear_shape& s)
-{
-    if (s.act == MP_ACT_NONE)
-        return 0;
-    return ((uint64_t)s.m * (uint64_t)s.n * (s.dtype == MP_F32 ? 4 : 2) + 15) / 16 * 16;
-}
+uint64_t linear_backward_ws_bytes(const mp_linear_shape& s) { return back_ws(s).bytes; }
 
 }  // namespace mp

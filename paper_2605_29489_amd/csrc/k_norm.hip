@@ -217,7 +217,7 @@ constexpr int back_threads(int tpr) { return tpr < 512 ? 512 : tpr; }
 // workgroup takes every gridDim-th band of rows; a thread keeps the sums of its
 // columns in registers (NV * V <= 16 columns, so that two rows and the sums
 // fit), the workgroup adds its bands' sums through LDS and writes one partial
-// row, which k_norm_part adds.  The next row is loaded before the present one
+// row, which k_sum_rows adds.  The next row is loaded before the present one
 // is reduced.
 template <int DT, int TPR, int NV>
 __global__ __launch_bounds__(back_threads(TPR)) void k_norm_back(NormBackArgs<DT> a)
@@ -367,29 +367,30 @@ __global__ __launch_bounds__(back_threads(TPR)) void k_norm_back(NormBackArgs<DT
     }
 }
 
-// Sum of n partial rows: 32 columns by 32 parts of the rows per workgroup.
-// blockIdx.y: 0 the weight's gradient, 1 the bias's.
+// Sum of n partial rows, `next` floats apart: 32 columns by 32 parts of the
+// rows per workgroup.  blockIdx.y picks the output, whose rows start y * pitch in.
 template <int DT>
-__global__ __launch_bounds__(1024) void k_norm_part(const float* part, int n, int pitch, int cols,
-                                                    typename Elem<DT>::T* dw, typename Elem<DT>::T* db)
+__global__ __launch_bounds__(1024) void k_sum_rows(const float* part, int n, int64_t next, int64_t pitch, int64_t cols,
+                                                   typename Elem<DT>::T* o0, typename Elem<DT>::T* o1)
 {
     __shared__ float t[32][33];
-    typename Elem<DT>::T* out = blockIdx.y ? db : dw;
+    typename Elem<DT>::T* out = blockIdx.y ? o1 : o0;
     if (!out)
         return;
-    const int c = threadIdx.x & 31, g = threadIdx.x >> 5, at = blockIdx.x * 32 + c;
+    const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
+    const int64_t at = (int64_t)blockIdx.x * 32 + c;
     float s = 0.0f;
     if (at < cols)
         for (int k = g; k < n; k += 32)
-            s += part[((int64_t)k * 2 + blockIdx.y) * pitch + at];
+            s += part[k * next + blockIdx.y * pitch + at];
     t[g][c] = s;
     __syncthreads();
     s = t[c][g];  // the parts of column g
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         s += __shfl_xor(s, o, 32);
-    if (c == 0 && blockIdx.x * 32 + g < cols)
-        out[blockIdx.x * 32 + g] = (typename Elem<DT>::T)s;
+    if (c == 0 && (int64_t)blockIdx.x * 32 + g < cols)
+        out[(int64_t)blockIdx.x * 32 + g] = (typename Elem<DT>::T)s;
 }
 
 // Rows longer than the one-pass kernel holds: dx, a workgroup per row.
@@ -563,8 +564,8 @@ hipError_t norm_back_t(const mp_norm_shape& s, const void* dy, const void* x, co
         }
     }
     if (cols)
-        hipLaunchKernelGGL(k_norm_part<DT>, dim3((unsigned)((s.cols + 31) / 32), 2), dim3(1024), 0, st,
-                           (const float*)ws, groups, pitch, (int)s.cols, (T*)dw, (T*)db);
+        hipLaunchKernelGGL(k_sum_rows<DT>, dim3((unsigned)((s.cols + 31) / 32), 2), dim3(1024), 0, st,
+                           (const float*)ws, groups, (int64_t)2 * pitch, (int64_t)pitch, s.cols, (T*)dw, (T*)db);
     return hipGetLastError();
 }
 
@@ -584,6 +585,18 @@ hipError_t launch_norm_backward(const mp_norm_shape& s, const void* dy, const vo
     return s.dtype == MP_F32
                ? norm_back_t<MP_F32>(s, dy, x, weight, mean, rstd, dx, lddx, dweight, dbias, ws, st)
                : norm_back_t<MP_BF16>(s, dy, x, weight, mean, rstd, dx, lddx, dweight, dbias, ws, st);
+}
+
+hipError_t launch_sum_rows(int dtype, const float* part, int n, int64_t pitch, int64_t cols, void* out, hipStream_t st)
+{
+    const dim3 g((unsigned)((cols + 31) / 32), 1);
+    if (dtype == MP_F32)
+        hipLaunchKernelGGL(k_sum_rows<MP_F32>, g, dim3(1024), 0, st, part, n, pitch, (int64_t)0, cols, (float*)out,
+                           nullptr);
+    else
+        hipLaunchKernelGGL(k_sum_rows<MP_BF16>, g, dim3(1024), 0, st, part, n, pitch, (int64_t)0, cols, (__bf16*)out,
+                           nullptr);
+    return hipGetLastError();
 }
 
 uint64_t norm_ws_bytes(const mp_norm_shape& s)

@@ -276,6 +276,10 @@ hipError_t launch_norm_backward(const mp_norm_shape& s, const void* dy, const vo
                                 void* dbias, void* ws, hipStream_t st);
 uint64_t norm_ws_bytes(const mp_norm_shape& s);
 
+// out[j] = sum of n partial rows of floats, `pitch` apart (k_norm.hip).
+hipError_t launch_sum_rows(int dtype, const float* part, int n, int64_t pitch, int64_t cols, void* out,
+                           hipStream_t st);
+
 // A few tokens through E experts (k_moe.hip).
 constexpr int kMoeMaxTokens = 64, kMoeMaxTop = 8;
 struct MoeArgs {
