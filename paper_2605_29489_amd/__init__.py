@@ -14,6 +14,7 @@ ImportError -- there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -226,6 +227,9 @@ def _floats(xs, K):
 def _stream(stream):
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle alone: 0.3 us against 3
+        if raw is not None:
+            return C.c_void_p(raw(torch.cuda.current_device()))
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return C.c_void_p(stream)
@@ -424,11 +428,8 @@ def _linear_shape(dtype, act, m, n, k, ldx=0, ldw=0, ldy=0, ldz=0, ldr=0):
     return mp_linear_shape(dtype, int(act), m, n, k, ldx, ldw, ldy, ldz, ldr)
 
 
-_WORD = C.c_uint64
-
-
 def _need(fn, *args) -> int:
-    n = _WORD(0)
+    n = C.c_uint64(0)
     _check(fn(*args, C.byref(n)))
     return n.value
 
@@ -447,7 +448,7 @@ def mp_linear(x, w, y, bias=None, residual=None, act: int = MP_ACT_NONE, z=None,
                       0 if residual is None else _matrix(residual, m, n, dt, "residual"))
     _vector(bias, n, dt, "bias")
     ref = C.byref(s)
-    wp, wb, hold = _scratch(_need(lib.mp_linear_workspace, ref, 0), workspace, x, stream)
+    wp, wb, hold = _scratch(mp_linear_workspace(s.dtype, s.act, m, n, k), workspace, x, stream)
     _check(lib.mp_linear(ref, x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(residual), y.data_ptr(), _ptr(z), wp, wb,
                          _stream(stream)))
 
@@ -472,12 +473,13 @@ def mp_linear_backward(dy, x=None, w=None, z=None, act: int = MP_ACT_NONE, dx=No
     lddw = 0 if dw is None else _matrix(dw, n, k, dt, "dw")
     _vector(dbias, n, dt, "dbias")
     ref = C.byref(s)
-    wp, wb, hold = _scratch(_need(lib.mp_linear_workspace, ref, 1), workspace, dy, stream)
+    wp, wb, hold = _scratch(mp_linear_workspace(s.dtype, s.act, m, n, k, True), workspace, dy, stream)
     _check(lib.mp_linear_backward(ref, dy.data_ptr(), _ptr(x) if dw is not None else None,
                                   _ptr(w) if dx is not None else None, _ptr(z) if act != MP_ACT_NONE else None,
                                   _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), wp, wb, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def mp_linear_workspace(dtype: int, act: int, m: int, n: int, k: int, backward: bool = False) -> int:
     s = _linear_shape(dtype, act, m, n, k)
     return _need(lib.mp_linear_workspace, C.byref(s), int(backward))
@@ -519,11 +521,12 @@ def mp_norm_backward(dy, x, rstd, mean=None, weight=None, rms: bool = False, dx=
     if mean is None and not rms:
         raise ValueError("layer norm needs mean")
     ref = C.byref(s)
-    wp, wb, hold = _scratch(_need(lib.mp_norm_workspace, ref), workspace, x, stream)
+    wp, wb, hold = _scratch(mp_norm_workspace(s.dtype, rows, cols, rms), workspace, x, stream)
     _check(lib.mp_norm_backward(ref, dy.data_ptr(), x.data_ptr(), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx), lddx,
                                 _ptr(dweight), _ptr(dbias), wp, wb, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def mp_norm_workspace(dtype: int, rows: int, cols: int, rms: bool = False) -> int:
     s = mp_norm_shape(dtype, MP_NORM_RMS if rms else 0, rows, cols, cols, cols, 0.0)
     return _need(lib.mp_norm_workspace, C.byref(s))

@@ -3,84 +3,138 @@
 #include "gemm.h"
 #include "mm_few.h"
 #include "mp_internal.h"
+#include <cstdlib>
 
 namespace mp {
 namespace {
 
 // ---------------------------------------------------------------- a few tokens
-// A workgroup takes NA tiles of 16 weight rows, its W waves split k, and the
+// A workgroup takes NA tiles of R weight rows, its W waves split k, and the
 // partial tiles meet in LDS.
-template <int DT, int NA, int TT, int W>
+template <int DT, int R, int NA, int TT, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_few(const char* x, int64_t ldx, const char* w, int64_t ldw,
                                                        typename Elem<DT>::T* y, int64_t ldy, int M, int64_t N,
                                                        int64_t K, Epi e)
 {
     using T = typename Elem<DT>::T;
+    using F = Few<DT, R, NA, TT, 1>;
     constexpr int es = Fmt<DT>::esize;
     __shared__ float4 red[W * NA * TT * 64];
     const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * NA), whole = few_whole<DT>(K);
-    const char *wp[NA], *xp[TT];
-    bool go[TT];
+    const int64_t n0 = (int64_t)blockIdx.x * (R * NA), whole = F::whole(K);
+    F f;
+    f.clear();
 #pragma unroll
-    for (int i = 0; i < NA; ++i) {  // rows past the last repeat it; their outputs are dropped
-        const int64_t r = n0 + i * 16 + (lane & 15);
-        wp[i] = w + (r < N ? r : N - 1) * ldw * es + (lane >> 4) * 16;
+    for (int i = 0; i < NA; ++i) {  // rows and tokens past the last repeat it; their outputs are dropped
+        const int64_t r = n0 + i * R + F::row_of(lane);
+        f.w[i] = w + (r < N ? r : N - 1) * ldw * es + F::w_off(lane);
     }
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
         const int r = t * 16 + (lane & 15);
-        go[t] = r < M;
-        xp[t] = go[t] ? x + (int64_t)r * ldx * es + (lane >> 4) * 16 : reinterpret_cast<const char*>(g_zero_steps);
+        f.x[t] = x + (int64_t)(r < M ? r : M - 1) * ldx * es + F::x_off(lane);
     }
-    f32x4 acc[NA][TT] = {};
-    few_steps<DT, NA, TT, 1, few_unroll(NA + TT)>(acc, wp, xp, go, whole * wave / W, whole * (wave + 1) / W);
-    if (wave == W - 1 && few_rest<DT>(K))
-        few_tail<DT, NA, TT, 1>(acc, wp, xp, go, whole, few_rest<DT>(K));
+    f.rounds(whole * wave / W, whole * (wave + 1) / W);
+    if (wave == W - 1 && F::more(K))
+        f.rest(K);
 #pragma unroll
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int t = 0; t < TT; ++t)
-            red[((wave * NA + i) * TT + t) * 64 + lane] =
-                make_float4(acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]);
+            red[((wave * NA + i) * TT + t) * 64 + lane] = f.out(i, t);
     __syncthreads();
-    sum_tiles<NA * TT>(red, W, threadIdx.x, 64 * W, [&](int q, const float4& s) {
-        const int t = (q >> 6) % TT * 16 + (q & 15);
-        const int64_t j0 = n0 + (q >> 6) / TT * 16 + ((q & 63) >> 4) * 4;
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        if (t >= M)
+    sum_tiles<R, NA * TT, W>(red, threadIdx.x, 64 * W, [&](int tile, int row, int tok, float v) {
+        const int t = tile % TT * 16 + tok;
+        const int64_t j = n0 + tile / TT * R + row;
+        if (t >= M || j >= N)
             return;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t j = j0 + u;
-            if (j >= N)
-                break;
-            float z = v[u];
-            if (e.bias)
-                z += (float)static_cast<const T*>(e.bias)[j];
-            if (e.z)
-                static_cast<T*>(e.z)[t * e.ldz + j] = (T)z;
-            float a = act_of(e.act, z);
-            if (e.r)
-                a += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
-            y[t * ldy + j] = (T)a;
-        }
+        if (e.bias)
+            v += (float)static_cast<const T*>(e.bias)[j];
+        if (e.z)
+            static_cast<T*>(e.z)[t * e.ldz + j] = (T)v;
+        v = act_of(e.act, v);
+        if (e.r)
+            v += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
+        y[t * ldy + j] = (T)v;
     });
+}
+
+// One to four tokens: a workgroup takes RG rows, its W waves split k.
+template <int DT, int RG, int TT, int W>
+__global__ __launch_bounds__(64 * W) void k_linear_gemv(const char* x, int64_t ldx, const char* w, int64_t ldw,
+                                                        typename Elem<DT>::T* y, int64_t ldy, int M, int64_t N,
+                                                        int64_t K, Epi e)
+{
+    using T = typename Elem<DT>::T;
+    using G = Gemv<DT, RG, TT, false>;
+    __shared__ float red[W][RG * TT];
+    const int wave = (int)uniform_u32(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * RG;
+    const char *wp[RG], *xp[TT];
+#pragma unroll
+    for (int i = 0; i < RG; ++i)  // rows and tokens past the last repeat it; their outputs are dropped
+        wp[i] = w + (n0 + i < N ? n0 + i : N - 1) * ldw * G::es;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+        xp[t] = x + (int64_t)(t < M ? t : M - 1) * ldx * G::es;
+    G g;
+    g.clear();
+    g.row(wp, xp, K, wave, W);
+    g.put(red[wave]);
+    __syncthreads();
+    const int t = threadIdx.x % TT;
+    const int64_t j = n0 + threadIdx.x / TT;
+    if (threadIdx.x >= RG * TT || t >= M || j >= N)
+        return;
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+        v += red[k][threadIdx.x];
+    if (e.bias)
+        v += (float)static_cast<const T*>(e.bias)[j];
+    if (e.z)
+        static_cast<T*>(e.z)[t * e.ldz + j] = (T)v;
+    v = act_of(e.act, v);
+    if (e.r)
+        v += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
+    y[t * ldy + j] = (T)v;
+}
+
+template <int DT, int RG, int TT>
+hipError_t gemv_go(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
+{
+    const int64_t groups = (s.n + RG - 1) / RG, runs = s.k / Gemv<DT, RG, TT, false>::kRun, want = 4096 / groups;
+    int64_t W = want < runs / 2 ? want : runs / 2;
+    if (const char* ev = getenv("FEW_W")) W = atoi(ev);
+    using T = typename Elem<DT>::T;
+#define MP_GEMV(w_)                                                                                               \
+    hipLaunchKernelGGL((k_linear_gemv<DT, RG, TT, w_>), dim3((unsigned)groups), dim3(64 * w_), 0, st,             \
+                       (const char*)x, s.ldx, (const char*)w, s.ldw, (T*)y, s.ldy, (int)s.m, s.n, s.k, e)
+    if (W >= 8)
+        MP_GEMV(8);
+    else if (W >= 4)
+        MP_GEMV(4);
+    else if (W >= 2)
+        MP_GEMV(2);
+    else
+        MP_GEMV(1);
+#undef MP_GEMV
+    return hipGetLastError();
 }
 
 constexpr int kFewTokens = 64;
 
-template <int DT, int NA, int TT>
+template <int DT, int R, int NA, int TT>
 hipError_t few_go(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
 {
-    // waves to fill the chip, with 8 steps each at least
-    const int64_t tiles = (s.n + 16 * NA - 1) / (16 * NA), whole = few_whole<DT>(s.k);
-    const int64_t most = whole / 8, want = 4096 / tiles;
-    const int64_t W = want < most ? want : most;
+    // waves to fill the chip, with 512 bytes of each row at least
+    const int64_t tiles = (s.n + R * NA - 1) / (R * NA), most = s.k * Fmt<DT>::esize / 512, want = 4096 / tiles;
+    int64_t W = want < most ? want : most;
+    if (const char* ev = getenv("FEW_W")) W = atoi(ev);
     const dim3 g((unsigned)tiles);
     using T = typename Elem<DT>::T;
-#define MP_FEW(w_)                                                                                              \
-    hipLaunchKernelGGL((k_linear_few<DT, NA, TT, w_>), g, dim3(64 * w_), 0, st, (const char*)x, s.ldx,            \
+#define MP_FEW(w_)                                                                                                \
+    hipLaunchKernelGGL((k_linear_few<DT, R, NA, TT, w_>), g, dim3(64 * w_), 0, st, (const char*)x, s.ldx,         \
                        (const char*)w, s.ldw, (T*)y, s.ldy, (int)s.m, s.n, s.k, e)
     if (W >= 16)
         MP_FEW(16);
@@ -95,11 +149,28 @@ hipError_t few_go(const mp_linear_shape& s, const void* x, const void* w, void* 
 template <int DT>
 hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
 {
-    if (s.m <= 16)
-        return few_go<DT, 1, 1>(s, x, w, y, e, st);
+    int RG = 4;
+    if (const char* ev = getenv("FEW_RG")) RG = atoi(ev);
+    if (s.m == 1 && RG == 4)
+        return gemv_go<DT, 4, 1>(s, x, w, y, e, st);
+    if (s.m == 1 && RG == 8)
+        return gemv_go<DT, 8, 1>(s, x, w, y, e, st);
+    if (s.m == 2 && RG)
+        return gemv_go<DT, 4, 2>(s, x, w, y, e, st);
+    if (s.m <= 4 && RG)
+        return gemv_go<DT, 4, 4>(s, x, w, y, e, st);
+    if (s.m <= 16) {
+        int R = s.n >= 8192 ? 16 : s.n >= 4096 ? 8 : 4;
+        if (const char* ev = getenv("FEW_R")) R = atoi(ev);
+        if (R == 16)
+            return few_go<DT, 16, 1, 1>(s, x, w, y, e, st);
+        if (R == 8)
+            return few_go<DT, 8, 1, 1>(s, x, w, y, e, st);
+        return few_go<DT, 4, 1, 1>(s, x, w, y, e, st);
+    }
     if (s.m <= 32)
-        return few_go<DT, 2, 2>(s, x, w, y, e, st);
-    return few_go<DT, 2, 4>(s, x, w, y, e, st);
+        return few_go<DT, 16, 2, 2>(s, x, w, y, e, st);
+    return few_go<DT, 16, 2, 4>(s, x, w, y, e, st);
 }
 
 // ---------------------------------------------------------------- dz
