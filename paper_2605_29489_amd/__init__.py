@@ -574,7 +574,8 @@ def mp_moe(layer: MoeLayer, x, router, experts, y, ids=None, gates=None, router_
             raise ValueError(f"experts: expected flat checkpoints of at least {need} values of {dt}")
     ref = C.byref(s)
     wp, wb, hold = _scratch(_need(lib.mp_moe_workspace, ref, T), workspace, x, stream)
-    _check(lib.mp_moe(ref, T, x.data_ptr(), ldx, router.data_ptr(), _ptr(router_bias), _ptrs(experts), E, residency,
+    ptrs = (C.c_void_p * max(E, 1))(*[e.data_ptr() for e in experts])
+    _check(lib.mp_moe(ref, T, x.data_ptr(), ldx, router.data_ptr(), _ptr(router_bias), ptrs, E, residency,
                       _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(ids), _ptr(gates), wp, wb, _stream(stream)))
 
 

@@ -361,7 +361,7 @@ struct Range {
 
 }  // namespace
 
-int check_device_buffer(const void* p, size_t bytes, const char* name)
+int check_device_buffer(const void* p, size_t bytes, const char* name, Allocation* seen)
 {
     if (p == nullptr)
         return fail(MP_E_ARG, "%s is NULL", name);
@@ -388,6 +388,8 @@ int check_device_buffer(const void* p, size_t bytes, const char* name)
         const char* q = static_cast<const char*>(p);
         if (q < b || (size_t)(q - b) + bytes > size)
             return fail(MP_E_ARG, "%s: %zu bytes needed, allocation too small", name, bytes);
+        if (seen != nullptr)
+            *seen = Allocation{b, size};
     } else {
         (void)hipGetLastError();
     }

@@ -3,61 +3,63 @@
 #include "gemm.h"
 #include "mm_few.h"
 #include "mp_internal.h"
-#include <cstdlib>
 
 namespace mp {
 namespace {
 
 // ---------------------------------------------------------------- a few tokens
-// A workgroup takes NA tiles of R weight rows, its W waves split k, and the
-// partial tiles meet in LDS.
-template <int DT, int R, int NA, int TT, int W>
+// A workgroup takes 16 weight rows, its W waves split k, and the partial tiles
+// meet in LDS.
+template <int DT, int T8, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_few(const char* x, int64_t ldx, const char* w, int64_t ldw,
                                                        typename Elem<DT>::T* y, int64_t ldy, int M, int64_t N,
                                                        int64_t K, Epi e)
 {
     using T = typename Elem<DT>::T;
-    using F = Few<DT, R, NA, TT, 1>;
+    using F = Few<DT, 1, T8, 1>;
     constexpr int es = Fmt<DT>::esize;
-    __shared__ float4 red[W * NA * TT * 64];
+    // a wave's operands on the way, then its partial tiles
+    constexpr int kWave = F::kLds > F::NT * 1024 ? F::kLds : F::NT * 1024;
+    __shared__ __attribute__((aligned(16))) char lds[W * kWave];
     const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * (R * NA), whole = F::whole(K);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
     F f;
     f.clear();
+    f.lds = lds + wave * kWave;
 #pragma unroll
-    for (int i = 0; i < NA; ++i) {  // rows and tokens past the last repeat it; their outputs are dropped
-        const int64_t r = n0 + i * R + F::row_of(lane);
-        f.w[i] = w + (r < N ? r : N - 1) * ldw * es + F::w_off(lane);
+    for (int m = 0; m < 2; ++m) {  // rows and tokens past the last repeat it; their outputs are dropped
+        const int64_t r = n0 + F::row_of(lane, m);
+        f.w[0][m] = w + (r < N ? r : N - 1) * ldw * es + F::off(lane);
     }
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        const int r = t * 16 + (lane & 15);
-        f.x[t] = x + (int64_t)(r < M ? r : M - 1) * ldx * es + F::x_off(lane);
+    for (int m = 0; m < T8; ++m) {
+        const int r = F::row_of(lane, m);
+        f.x[0][m] = x + (int64_t)(r < M ? r : M - 1) * ldx * es + F::off(lane);
     }
-    f.rounds(whole * wave / W, whole * (wave + 1) / W);
-    if (wave == W - 1 && F::more(K))
-        f.rest(K);
+    f.row(K, wave, W);
+    float4* red = reinterpret_cast<float4*>(f.lds);
 #pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-            red[((wave * NA + i) * TT + t) * 64 + lane] = f.out(i, t);
+    for (int t = 0; t < F::NT; ++t)
+        red[t * 64 + lane] = f.out(0, t);
     __syncthreads();
-    sum_tiles<R, NA * TT, W>(red, threadIdx.x, 64 * W, [&](int tile, int row, int tok, float v) {
-        const int t = tile % TT * 16 + tok;
-        const int64_t j = n0 + tile / TT * R + row;
-        if (t >= M || j >= N)
-            return;
-        if (e.bias)
-            v += (float)static_cast<const T*>(e.bias)[j];
-        if (e.z)
-            static_cast<T*>(e.z)[t * e.ldz + j] = (T)v;
-        v = act_of(e.act, v);
-        if (e.r)
-            v += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
-        y[t * ldy + j] = (T)v;
-    });
+    sum_tiles<F::NT, W>(reinterpret_cast<const float4*>(lds), kWave / 16, threadIdx.x, 64 * W,
+                        [&](int tile, int row, int tok, float v) {
+                            const int t = tile * 16 + tok;
+                            const int64_t j = n0 + row;
+                            if (t >= M || j >= N)
+                                return;
+                            if (e.bias)
+                                v += (float)static_cast<const T*>(e.bias)[j];
+                            if (e.z)
+                                static_cast<T*>(e.z)[t * e.ldz + j] = (T)v;
+                            v = act_of(e.act, v);
+                            if (e.r)
+                                v += (float)static_cast<const T*>(e.r)[t * e.ldr + j];
+                            y[t * ldy + j] = (T)v;
+                        });
 }
+
+constexpr int kFewTokens = 64;
 
 // One to four tokens: a workgroup takes RG rows, its W waves split k.
 template <int DT, int RG, int TT, int W>
@@ -104,8 +106,7 @@ template <int DT, int RG, int TT>
 hipError_t gemv_go(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
 {
     const int64_t groups = (s.n + RG - 1) / RG, runs = s.k / Gemv<DT, RG, TT, false>::kRun, want = 4096 / groups;
-    int64_t W = want < runs / 2 ? want : runs / 2;
-    if (const char* ev = getenv("FEW_W")) W = atoi(ev);
+    const int64_t W = want < runs / 2 ? want : runs / 2;
     using T = typename Elem<DT>::T;
 #define MP_GEMV(w_)                                                                                               \
     hipLaunchKernelGGL((k_linear_gemv<DT, RG, TT, w_>), dim3((unsigned)groups), dim3(64 * w_), 0, st,             \
@@ -122,23 +123,24 @@ hipError_t gemv_go(const mp_linear_shape& s, const void* x, const void* w, void*
     return hipGetLastError();
 }
 
-constexpr int kFewTokens = 64;
 
-template <int DT, int R, int NA, int TT>
+template <int DT, int T8>
 hipError_t few_go(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
 {
     // waves to fill the chip, with 512 bytes of each row at least
-    const int64_t tiles = (s.n + R * NA - 1) / (R * NA), most = s.k * Fmt<DT>::esize / 512, want = 4096 / tiles;
-    int64_t W = want < most ? want : most;
-    if (const char* ev = getenv("FEW_W")) W = atoi(ev);
+    const int64_t tiles = (s.n + 15) / 16, most = s.k * Fmt<DT>::esize / 512, want = 4096 / tiles;
+    const int64_t W = want < most ? want : most;
     const dim3 g((unsigned)tiles);
     using T = typename Elem<DT>::T;
 #define MP_FEW(w_)                                                                                                \
-    hipLaunchKernelGGL((k_linear_few<DT, R, NA, TT, w_>), g, dim3(64 * w_), 0, st, (const char*)x, s.ldx,         \
+    hipLaunchKernelGGL((k_linear_few<DT, T8, w_>), g, dim3(64 * w_), 0, st, (const char*)x, s.ldx,            \
                        (const char*)w, s.ldw, (T*)y, s.ldy, (int)s.m, s.n, s.k, e)
-    if (W >= 16)
-        MP_FEW(16);
-    else if (W >= 8)
+    if constexpr (T8 < 8)
+        if (W >= 16) {
+            MP_FEW(16);
+            return hipGetLastError();
+        }
+    if (W >= 8)
         MP_FEW(8);
     else
         MP_FEW(4);
@@ -149,28 +151,19 @@ hipError_t few_go(const mp_linear_shape& s, const void* x, const void* w, void* 
 template <int DT>
 hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, void* y, const Epi& e, hipStream_t st)
 {
-    int RG = 4;
-    if (const char* ev = getenv("FEW_RG")) RG = atoi(ev);
-    if (s.m == 1 && RG == 4)
+    if (s.m == 1)
         return gemv_go<DT, 4, 1>(s, x, w, y, e, st);
-    if (s.m == 1 && RG == 8)
-        return gemv_go<DT, 8, 1>(s, x, w, y, e, st);
-    if (s.m == 2 && RG)
+    if (s.m == 2)
         return gemv_go<DT, 4, 2>(s, x, w, y, e, st);
-    if (s.m <= 4 && RG)
+    if (s.m <= 4)
         return gemv_go<DT, 4, 4>(s, x, w, y, e, st);
-    if (s.m <= 16) {
-        int R = s.n >= 8192 ? 16 : s.n >= 4096 ? 8 : 4;
-        if (const char* ev = getenv("FEW_R")) R = atoi(ev);
-        if (R == 16)
-            return few_go<DT, 16, 1, 1>(s, x, w, y, e, st);
-        if (R == 8)
-            return few_go<DT, 8, 1, 1>(s, x, w, y, e, st);
-        return few_go<DT, 4, 1, 1>(s, x, w, y, e, st);
-    }
+    if (s.m <= 8)
+        return few_go<DT, 1>(s, x, w, y, e, st);
+    if (s.m <= 16)
+        return few_go<DT, 2>(s, x, w, y, e, st);
     if (s.m <= 32)
-        return few_go<DT, 16, 2, 2>(s, x, w, y, e, st);
-    return few_go<DT, 16, 2, 4>(s, x, w, y, e, st);
+        return few_go<DT, 4>(s, x, w, y, e, st);
+    return few_go<DT, 8>(s, x, w, y, e, st);
 }
 
 // ---------------------------------------------------------------- dz

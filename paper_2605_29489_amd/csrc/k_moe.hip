@@ -3,7 +3,6 @@
 #include "ffn_common.h"
 #include "mm_few.h"
 #include "mp_internal.h"
-#include <cstdlib>
 
 namespace mp {
 namespace {
@@ -15,7 +14,8 @@ struct Routing {
     uint8_t slot[kMaxK][kMoeMaxTokens];  // choice number of expert e for token t, or kNone
     uint8_t list[kMaxK][kMoeMaxTokens];  // the tokens that have expert e, in order
     uint32_t count[kMaxK];               // how many
-    uint32_t reached;                    // experts that some token has
+    uint32_t unit[2 * kMaxK];            // e + 256 (its first token's number / 32): up to 32 tokens of an expert
+    uint32_t units;
     uint32_t pad[3];
 };
 
@@ -38,12 +38,15 @@ __device__ inline T* h_row(T* h, const MoeArgs& a, const Routing& rt, int e, int
     return h + ((int64_t)t * a.l.top_k + rt.slot[e][t]) * pitch;
 }
 
-// The expert number k of those reached.
-__device__ inline int nth_expert(uint32_t reached, int64_t k)
+// Unit u: its expert, its first token's number among the expert's, how many tokens.
+struct Unit {
+    int e, first, n;
+};
+__device__ inline Unit unit_of(const Routing& rt, int u)
 {
-    for (; k > 0; --k)
-        reached &= reached - 1;
-    return __ffs(reached) - 1;
+    const uint32_t v = uniform_u32(rt.unit[u]);
+    const int e = (int)(v & 255), first = (int)(v >> 8) * 32, c = (int)uniform_u32(rt.count[e]) - first;
+    return Unit{e, first, c < 32 ? c : 32};
 }
 
 constexpr int kUpWaves = 8, kUpThreads = 64 * kUpWaves;
@@ -109,9 +112,16 @@ __device__ inline void choose_experts(const MoeArgs& a, Routing* rt, float (*gat
     }
     __syncthreads();
     if (wave == 0) {
-        const unsigned long long m = __ballot(lane < kMaxK && rt->count[lane & 31] != 0);
+        const uint32_t c = lane < kMaxK ? rt->count[lane] : 0;
+        const unsigned long long m1 = __ballot(c > 0), m2 = __ballot(c > 32);
+        const unsigned long long below = (1ull << lane) - 1;
+        const int at = __popcll(m1 & below) + __popcll(m2 & below);
+        if (c > 0)
+            rt->unit[at] = lane;
+        if (c > 32)
+            rt->unit[at + 1] = lane + 256;
         if (lane == 0)
-            rt->reached = (uint32_t)m;
+            rt->units = (uint32_t)(__popcll(m1) + __popcll(m2));
     }
     __syncthreads();
 }
@@ -120,36 +130,44 @@ __device__ inline void choose_experts(const MoeArgs& a, Routing* rt, float (*gat
 // instructions, so that the gate and up products need no launch of their own
 // behind it.  lg: 32 floats of LDS per token (of whole token tiles); red: LDS
 // for the partial tiles.
-template <int DT, int TT>
-__device__ inline void logits_tiles(const MoeArgs& a, float* lg, float4* red)
+template <int DT, int T8>
+__device__ inline void logits_tiles(const MoeArgs& a, float* lg, char* lds, int per_wave)
 {
     using T = typename Elem<DT>::T;
+    using F = Few<DT, 1, T8, 1>;
     const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
-    using F = Few<DT, 16, 1, TT, 1>;
-    const int64_t D = a.l.hidden, whole = F::whole(D);
+    const int64_t D = a.l.hidden;
     F f;
+    f.lds = lds + wave * per_wave;
+    for (int t0 = 0; t0 < a.T; t0 += T8 * 8)
+        for (int e0 = 0; e0 < a.E; e0 += 16) {
+            f.clear();
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        const int tok = t * 16 + (lane & 15);
-        f.x[t] = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + (int64_t)(tok < a.T ? tok : a.T - 1) * a.ldx) +
-                 F::x_off(lane);
-    }
-    for (int e0 = 0; e0 < a.E; e0 += 16) {
-        f.clear();
-        const int e = e0 + F::row_of(lane);
-        f.w[0] = reinterpret_cast<const char*>(static_cast<const T*>(a.router) + (e < a.E ? e : a.E - 1) * D) +
-                 F::w_off(lane);
-        f.rounds(whole * wave / kUpWaves, whole * (wave + 1) / kUpWaves);
-        if (wave == kUpWaves - 1 && F::more(D))
-            f.rest(D);
+            for (int m = 0; m < T8; ++m) {
+                const int tok = t0 + F::row_of(lane, m);
+                f.x[0][m] = reinterpret_cast<const char*>(static_cast<const T*>(a.x) +
+                                                          (int64_t)(tok < a.T ? tok : a.T - 1) * a.ldx) +
+                            F::off(lane);
+            }
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-            red[(wave * TT + t) * 64 + lane] = f.out(0, t);
-        __syncthreads();
-        sum_tiles<16, TT, kUpWaves>(red, threadIdx.x, kUpThreads,
-                                    [&](int t, int row, int tok, float v) { lg[(t * 16 + tok) * 32 + e0 + row] = v; });
-        __syncthreads();
-    }
+            for (int m = 0; m < 2; ++m) {
+                const int e = e0 + F::row_of(lane, m);
+                f.w[0][m] =
+                    reinterpret_cast<const char*>(static_cast<const T*>(a.router) + (e < a.E ? e : a.E - 1) * D) +
+                    F::off(lane);
+            }
+            f.row(D, wave, kUpWaves);
+#pragma unroll
+            for (int t = 0; t < F::NT; ++t)
+                reinterpret_cast<float4*>(f.lds)[t * 64 + lane] = f.out(0, t);
+            __syncthreads();
+            sum_tiles<F::NT, kUpWaves>(reinterpret_cast<const float4*>(lds), per_wave / 16, threadIdx.x, kUpThreads,
+                                       [&](int t, int row, int tok, float v) {
+                                           if (t0 + t * 16 + tok < kMoeMaxTokens)
+                                               lg[(t0 + t * 16 + tok) * 32 + e0 + row] = v;
+                                       });
+            __syncthreads();
+        }
 }
 
 // The same for one to four tokens, a wave per router row.
@@ -186,6 +204,47 @@ __device__ inline void pass_on(const Routing& rt, Routing* out)
             reinterpret_cast<uint32_t*>(out)[i] = reinterpret_cast<const uint32_t*>(&rt)[i];
 }
 
+template <int DT>
+__device__ inline void put_y(const MoeArgs& a, int tok, int64_t d, float y)
+{
+    using T = typename Elem<DT>::T;
+    if (a.residual)
+        y += (float)static_cast<const T*>(a.residual)[tok * a.ldr + d];
+    static_cast<T*>(a.y)[tok * a.ldy + d] = (T)y;
+}
+
+// A workgroup's sums part(tok, row) of the rows from d0 on: into y, or, where
+// several workgroups split the contraction, into parts[split][token][hidden].
+template <int DT, int ROWS, typename F>
+__device__ inline void finish_rows(const MoeArgs& a, int64_t d0, int split, int splits, float* parts, F part)
+{
+    for (int q = threadIdx.x; q < a.T * ROWS; q += blockDim.x) {
+        const int tok = q / ROWS;
+        const int64_t d = d0 + q % ROWS;
+        if (d >= a.l.hidden)
+            continue;
+        const float s = part(tok, q % ROWS);
+        if (splits > 1)
+            parts[((int64_t)split * a.T + tok) * a.l.hidden + d] = s;
+        else
+            put_y<DT>(a, tok, d, s);
+    }
+}
+
+// y from the parts: only where hidden is so small that its row groups leave
+// CUs without work.
+template <int DT>
+__global__ __launch_bounds__(256) void k_moe_join(MoeArgs a, const float* parts, int splits)
+{
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.T * a.l.hidden;
+    if (q >= n)
+        return;
+    float y = 0.0f;
+    for (int s = 0; s < splits; ++s)
+        y += parts[s * n + q];
+    put_y<DT>(a, (int)(q / a.l.hidden), q % a.l.hidden, y);
+}
+
 // act(g) * u * gate
 __device__ inline float hidden_of(const MoeArgs& a, float g, float u, float gate)
 {
@@ -194,24 +253,39 @@ __device__ inline float hidden_of(const MoeArgs& a, float g, float u, float gate
 }
 
 // ---------------------------------------------------------------- five tokens and more
-// h = act(gate x) * (up x) times the token's gate for every (expert that a
-// token has, 16 rows of ffn): WS waves split an item's contraction.  The B
-// operand's columns are the expert's tokens, up to 16 TT of them.  h is stored
-// as one value (fp32) or as the bf16 rounding and the rounded remainder, in two
-// planes.
-template <int DT, int TT, int WS>
-__global__ __launch_bounds__(kUpThreads, 4) void k_moe_up(MoeArgs a, ExpertPtrs ex, Routing* out, char* hbuf)
+// Calls go(eights) for the template value that covers n tokens, up to T8.
+template <int T8, typename F>
+__device__ inline void with_eights(int n, F go)
+{
+    if (n <= 8)
+        go(std::integral_constant<int, 1>{});
+    else if (T8 == 2 || n <= 16)
+        go(std::integral_constant<int, T8 < 2 ? 1 : 2>{});
+    else
+        go(std::integral_constant<int, T8>{});
+}
+
+// h = act(gate x) * (up x) times the token's gate for every (unit, 16 rows of
+// ffn): WS waves split an item's contraction.  The B operand's columns are the
+// unit's tokens.  h is stored as one value (fp32) or as the bf16 rounding and
+// the rounded remainder, in two planes.
+template <int DT, int T8, int WS>
+__global__ __launch_bounds__(kUpThreads, T8 == 4 ? 2 : 4) void k_moe_up(MoeArgs a, ExpertPtrs ex, Routing* out, char* hbuf)
 {
     using T = typename Elem<DT>::T;
+    constexpr int NT = (T8 + 1) / 2;
+    constexpr int kWave = Few<DT, 2, T8, 1>::kLds;  // a wave's operands on the way, then its partial tiles
+    static_assert(kWave >= 2 * NT * 1024);
     __shared__ Routing rt;
     __shared__ float gate[kMoeMaxTokens][kMoeMaxTop];
-    __shared__ float4 red[kUpWaves * 2 * TT * 64];
+    __shared__ float lg[kMoeMaxTokens * 32];
+    __shared__ __attribute__((aligned(16))) char lds[kUpWaves * kWave];
     const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
-    logits_tiles<DT, TT>(a, reinterpret_cast<float*>(red + kUpWaves * TT * 64), red);
-    choose_experts<DT>(a, &rt, gate, reinterpret_cast<float*>(red + kUpWaves * TT * 64));
+    logits_tiles<DT, T8>(a, lg, lds, kWave);
+    choose_experts<DT>(a, &rt, gate, lg);
     pass_on(rt, out);
     const int64_t D = a.l.hidden, F = a.l.ffn, pitch = moe_pitch(F), plane = (int64_t)a.T * a.l.top_k * pitch;
-    const int64_t tiles = (F + 15) / 16, items = tiles * __popc(rt.reached);
+    const int64_t tiles = (F + 15) / 16, items = tiles * uniform_u32(rt.units);
     const int group = wave / WS, part = wave % WS;
     constexpr int kGroups = kUpWaves / WS;
     const bool two = a.l.up_off >= 0;
@@ -219,97 +293,75 @@ __global__ __launch_bounds__(kUpThreads, 4) void k_moe_up(MoeArgs a, ExpertPtrs 
     for (int64_t it0 = (int64_t)blockIdx.x * kGroups; it0 < items; it0 += (int64_t)gridDim.x * kGroups) {
         const int64_t it = it0 + group;
         const bool on = it < items;
-        const int e = on ? nth_expert(rt.reached, it / tiles) : 0;
+        const Unit u = unit_of(rt, on ? (int)(it / tiles) : 0);
         const int64_t f0 = on ? it % tiles * 16 : 0;
-        const int n = on ? (int)uniform_u32(rt.count[e]) : 0;
-        // outputs of token number `pos` of the expert, row f
-        auto put = [&](int pos, int64_t f, float g, float u) {
-            if (pos >= n || f >= F)
+        // outputs of token number `pos` of the unit, row f
+        auto put = [&](int pos, int64_t f, float g, float up) {
+            if (pos >= u.n || f >= F)
                 return;
-            const int tok = rt.list[e][pos];
-            const float h = hidden_of(a, g, u, gate[tok][rt.slot[e][tok]]);
-            T* p = h_row(reinterpret_cast<T*>(hbuf), a, rt, e, tok, pitch) + f;
+            const int tok = rt.list[u.e][u.first + pos];
+            const float h = hidden_of(a, g, up, gate[tok][rt.slot[u.e][tok]]);
+            T* p = h_row(reinterpret_cast<T*>(hbuf), a, rt, u.e, tok, pitch) + f;
             *p = (T)h;
             if constexpr (DT == MP_BF16) {
                 const float hi = (float)(T)h;
                 p[plane] = (T)(fabsf(hi) < INFINITY ? h - hi : 0.0f);  // an infinite or NaN h has no remainder
             }
         };
-        // the item with NT token tiles
-        auto work = [&](auto nt) {
-            constexpr int NT = decltype(nt)::value;
-            float4 sum[2][NT];  // gate and up
-            const int64_t row = f0 + (lane & 15) < F ? f0 + (lane & 15) : F - 1;
-            auto go = [&](auto& f, int na) {
-                using FW = std::remove_reference_t<decltype(f)>;
-                const char* const base =
-                    static_cast<const char*>(ex.p[e]) + row * D * Fmt<DT>::esize + FW::w_off(lane);
-                f.clear();
-                f.w[0] = base + a.l.gate_off * Fmt<DT>::esize;
-                if (na > 1)
-                    f.w[na - 1] = base + a.l.up_off * Fmt<DT>::esize;
+        float4* const red = reinterpret_cast<float4*>(lds + wave * kWave);  // [token tile][gate, up]
+        auto work = [&](auto eights, auto mats) {
+            constexpr int NA = decltype(mats)::value;
+            using FW = Few<DT, NA, decltype(eights)::value, 1>;
+            FW f;
+            f.clear();
+            f.lds = lds + wave * kWave;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {  // columns past the last token repeat it; their outputs are dropped
-                    const int pos = t * 16 + (lane & 15), tok = rt.list[e][pos < n ? pos : n - 1];
-                    f.x[t] = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + tok * a.ldx) + FW::x_off(lane);
-                }
-                const int64_t whole = FW::whole(D);
-                f.rounds(whole * part / WS, whole * (part + 1) / WS);
-                if (part == WS - 1 && FW::more(D))
-                    f.rest(D);
-            };
-            if (two) {
-                Few<DT, 16, 2, NT, 1> f;
-                go(f, 2);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    sum[0][t] = f.out(0, t);
-                    sum[1][t] = f.out(1, t);
-                }
-            } else {
-                Few<DT, 16, 1, NT, 1> f;
-                go(f, 1);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    sum[0][t] = f.out(0, t);
-                    sum[1][t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                }
+            for (int m = 0; m < 2; ++m) {
+                const int64_t r = f0 + FW::row_of(lane, m);
+                const char* base =
+                    static_cast<const char*>(ex.p[u.e]) + (r < F ? r : F - 1) * D * Fmt<DT>::esize + FW::off(lane);
+                f.w[0][m] = base + a.l.gate_off * Fmt<DT>::esize;
+                if constexpr (NA == 2)
+                    f.w[1][m] = base + a.l.up_off * Fmt<DT>::esize;
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int m = 0; m < decltype(eights)::value; ++m) {  // columns past the last token repeat it
+                const int pos = FW::row_of(lane, m), tok = rt.list[u.e][u.first + (pos < u.n ? pos : u.n - 1)];
+                f.x[0][m] = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + tok * a.ldx) + FW::off(lane);
+            }
+            f.row(D, part, WS);
+#pragma unroll
+            for (int t = 0; t < FW::NT; ++t) {
+                const float4 g = f.out(0, t), up = NA == 2 ? f.out(NA - 1, t) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if constexpr (WS == 1) {
-                    const float* g = reinterpret_cast<const float*>(&sum[0][t]);
-                    const float* u = reinterpret_cast<const float*>(&sum[1][t]);
+                    const float gv[4] = {g.x, g.y, g.z, g.w}, uv[4] = {up.x, up.y, up.z, up.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        put(t * 16 + (lane & 15), f0 + (lane >> 4) * 4 + j, g[j], u[j]);
+                        put(t * 16 + (lane & 15), f0 + (lane >> 4) * 4 + j, gv[j], uv[j]);
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        red[(((group * WS + part) * TT + t) * 2 + i) * 64 + lane] = sum[i][t];
+                    red[(t * 2 + 0) * 64 + lane] = g;
+                    red[(t * 2 + 1) * 64 + lane] = up;
                 }
             }
         };
-        const int nt = (n + 15) / 16;
-        if (nt == 1)
-            work(std::integral_constant<int, 1>{});
-        if constexpr (TT > 1)
-            if (nt == 2)
-                work(std::integral_constant<int, 2>{});
-        if constexpr (TT > 2)
-            if (nt > 2)
-                work(std::integral_constant<int, 4>{});
+        if (on)
+            with_eights<T8>(u.n, [&](auto eights) {
+                if (two)
+                    work(eights, std::integral_constant<int, 2>{});
+                else
+                    work(eights, std::integral_constant<int, 1>{});
+            });
         if constexpr (WS > 1) {
             __syncthreads();
-            const float* r = reinterpret_cast<const float*>(red + group * WS * TT * 128);
-            for (int q = part * 64 + lane; q < nt * 256; q += WS * 64) {  // float q % 256 of a token tile
+            const float* r = reinterpret_cast<const float*>(lds + group * WS * kWave);
+            for (int q = part * 64 + lane; on && q < (u.n + 15) / 16 * 256; q += WS * 64) {  // float q % 256 of a tile
                 const int t = q / 256, o = q % 256;
                 float s[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int w = 0; w < WS; ++w)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        s[i] += r[((w * TT + t) * 2 + i) * 256 + o];
+                        s[i] += r[w * (kWave / 4) + (t * 2 + i) * 256 + o];
                 put(t * 16 + o / 4 % 16, f0 + o / 64 * 4 + (o & 3), s[0], s[1]);
             }
             __syncthreads();
@@ -317,96 +369,83 @@ __global__ __launch_bounds__(kUpThreads, 4) void k_moe_up(MoeArgs a, ExpertPtrs 
     }
 }
 
-// y = residual + sum over the experts of down h: a workgroup takes 16 rows of
-// hidden, its waves split the contraction over (expert, ffn).  An expert's
-// columns are its tokens; behind its part of an expert a wave adds its sums to
-// its own row of LDS per token.
-template <int DT, int TT, int W>
-__global__ __launch_bounds__(64 * W) void k_moe_down(MoeArgs a, ExpertPtrs ex, const Routing* in, const char* hbuf)
+// y = residual + sum over the units of down h: a workgroup takes 16 rows of
+// hidden, its waves split the contraction over (unit, ffn).  A unit's columns
+// are its tokens; behind its part of a unit a wave adds its sums to its own row
+// of LDS per token.
+template <int DT, int T8, int W>
+__global__ __launch_bounds__(64 * W) void k_moe_down(MoeArgs a, ExpertPtrs ex, const Routing* in, const char* hbuf,
+                                                     float* parts, int splits)
 {
     using T = typename Elem<DT>::T;
-    constexpr int XS = DT == MP_BF16 ? 2 : 1;
+    constexpr int XS = DT == MP_BF16 ? 2 : 1, kTokens = T8 < 4 ? T8 * 8 : kMoeMaxTokens;
+    constexpr int kWave = Few<DT, 1, T8, XS>::kLds;
     __shared__ Routing rt;
-    __shared__ float4 sums[W][TT * 16][4];  // [token][4 of the 16 rows]
+    __shared__ float4 sums[W][kTokens][4];  // [token][4 of the 16 rows]
+    __shared__ __attribute__((aligned(16))) char lds[W * kWave];
     const int lane = threadIdx.x & 63, wave = (int)uniform_u32(threadIdx.x >> 6);
     for (int i = threadIdx.x; i < (int)(sizeof(Routing) / 4); i += 64 * W)
         reinterpret_cast<uint32_t*>(&rt)[i] = reinterpret_cast<const uint32_t*>(in)[i];
-    for (int i = lane; i < TT * 64; i += 64)
+    for (int i = lane; i < kTokens * 4; i += 64)
         sums[wave][i / 4][i % 4] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     __syncthreads();
     const int64_t D = a.l.hidden, F = a.l.ffn, pitch = moe_pitch(F);
     const int64_t plane = (int64_t)a.T * a.l.top_k * pitch;
-    const int64_t d0 = (int64_t)blockIdx.x * 16, row = d0 + (lane & 15) < D ? d0 + (lane & 15) : D - 1;
-    const uint32_t reached = uniform_u32(rt.reached);
-    const int n = __popc(reached);
-    // shares of the contraction in 256 bytes of a row
-    constexpr int kShare = 256 / Fmt<DT>::esize;
-    const int64_t shares = F / kShare, s0 = shares * n * wave / W, s1 = shares * n * (wave + 1) / W;
-    uint32_t left = reached;
-    for (int k = 0; k < n; ++k, left &= left - 1) {
+    const int grp = blockIdx.x / splits, split = blockIdx.x % splits;
+    const int64_t d0 = (int64_t)grp * 16;
+    const int n = (int)uniform_u32(rt.units), me = split * W + wave, all = splits * W;
+    // shares of the contraction: 4 blocks, a whole number of rounds for every count of tokens
+    constexpr int kShareBlocks = 4, kShare = kShareBlocks * 128 / Fmt<DT>::esize;
+    const int64_t shares = (F + kShare - 1) / kShare, s0 = shares * n * me / all, s1 = shares * n * (me + 1) / all;
+    for (int k = 0; k < n; ++k) {
         const int64_t lo = s0 > shares * k ? s0 - shares * k : 0;
         const int64_t hi = s1 < shares * (k + 1) ? s1 - shares * k : shares;
-        const bool rest = F % kShare && k % W == wave;
-        if (lo >= hi && !rest)
+        if (lo >= hi)
             continue;
-        const int e = __ffs(left) - 1, c = (int)uniform_u32(rt.count[e]);
-        auto work = [&](auto nt) {
-            constexpr int NT = decltype(nt)::value;
-            using FD = Few<DT, 16, 1, NT, XS>;
-            constexpr int kPer = 256 / (FD::kRound * FD::kStep);  // rounds of a share
-            static_assert(kPer >= 1);
+        const Unit u = unit_of(rt, k);
+        with_eights<T8>(u.n, [&](auto eights) {
+            constexpr int E8 = decltype(eights)::value;
+            using FD = Few<DT, 1, E8, XS>;
+            static_assert(kShareBlocks % FD::kRound == 0);
             FD f;
             f.clear();
-            f.w[0] = static_cast<const char*>(ex.p[e]) + (a.l.down_off + row * F) * Fmt<DT>::esize + FD::w_off(lane);
+            f.lds = lds + wave * kWave;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int pos = t * 16 + (lane & 15), tok = rt.list[e][pos < c ? pos : c - 1];
+            for (int m = 0; m < 2; ++m) {
+                const int64_t r = d0 + FD::row_of(lane, m);
+                f.w[0][m] = static_cast<const char*>(ex.p[u.e]) +
+                            (a.l.down_off + (r < D ? r : D - 1) * F) * Fmt<DT>::esize + FD::off(lane);
+            }
+#pragma unroll
+            for (int m = 0; m < E8; ++m) {
+                const int pos = FD::row_of(lane, m), tok = rt.list[u.e][u.first + (pos < u.n ? pos : u.n - 1)];
 #pragma unroll
                 for (int i = 0; i < XS; ++i)
-                    f.x[i * NT + t] = reinterpret_cast<const char*>(
-                                          h_row(reinterpret_cast<const T*>(hbuf) + i * plane, a, rt, e, tok, pitch)) +
-                                      FD::x_off(lane);
+                    f.x[i][m] = reinterpret_cast<const char*>(
+                                    h_row(reinterpret_cast<const T*>(hbuf) + i * plane, a, rt, u.e, tok, pitch)) +
+                                FD::off(lane);
             }
-            f.rounds(lo * kPer, hi * kPer);
-            if (rest) {  // behind the shares: rounds, steps, part of a step
-                f.rounds(shares * kPer, FD::whole(F));
-                if (FD::more(F))
-                    f.rest(F);
-            }
+            f.blocks(lo * kShareBlocks, hi * kShareBlocks, F);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < FD::NT; ++t) {
                 const int pos = t * 16 + (lane & 15);
-                if (pos < c) {
+                if (pos < u.n) {
                     const float4 v = f.out(0, t);
-                    float4& s = sums[wave][rt.list[e][pos]][lane >> 4];
+                    float4& s = sums[wave][rt.list[u.e][u.first + pos]][lane >> 4];
                     s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
                 }
             }
-        };
-        if (c <= 16)
-            work(std::integral_constant<int, 1>{});
-        if constexpr (TT > 1)
-            if (c > 16 && c <= 32)
-                work(std::integral_constant<int, 2>{});
-        if constexpr (TT > 2)
-            if (c > 32)
-                work(std::integral_constant<int, 4>{});
+        });
     }
     __syncthreads();
     const float* r = reinterpret_cast<const float*>(sums);
-    for (int q = threadIdx.x; q < a.T * 16; q += 64 * W) {
-        const int tok = q / 16;
-        const int64_t d = d0 + q % 16;
-        if (d >= D)
-            continue;
+    finish_rows<DT, 16>(a, d0, split, splits, parts, [&](int tok, int row) {
         float y = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w)
-            y += r[w * TT * 256 + q];
-        if (a.residual)
-            y += (float)static_cast<const T*>(a.residual)[tok * a.ldr + d];
-        static_cast<T*>(a.y)[tok * a.ldy + d] = (T)y;
-    }
+            y += r[w * kTokens * 16 + tok * 16 + row];
+        return y;
+    });
 }
 
 // ---------------------------------------------------------------- one to four tokens
@@ -426,16 +465,16 @@ __global__ __launch_bounds__(kUpThreads) void k_moe_up_gemv(MoeArgs a, ExpertPtr
     choose_experts<DT>(a, &rt, gate, lg);
     pass_on(rt, out);
     const int64_t D = a.l.hidden, F = a.l.ffn, pitch = moe_pitch(F);
-    const int64_t tiles = (F + kUpRows - 1) / kUpRows, items = tiles * __popc(uniform_u32(rt.reached));
+    const int64_t tiles = (F + kUpRows - 1) / kUpRows, items = tiles * uniform_u32(rt.units);
     const int group = wave / WS, part = wave % WS;
     constexpr int kGroups = kUpWaves / WS;
     const bool two = a.l.up_off >= 0;
     for (int64_t it0 = (int64_t)blockIdx.x * kGroups; it0 < items; it0 += (int64_t)gridDim.x * kGroups) {
         const int64_t it = it0 + group;
         const bool on = it < items;
-        const int e = on ? nth_expert(uniform_u32(rt.reached), it / tiles) : 0;
+        const Unit u = unit_of(rt, on ? (int)(it / tiles) : 0);
+        const int e = u.e, n = on ? u.n : 0;
         const int64_t f0 = on ? it % tiles * kUpRows : 0;
-        const int n = on ? (int)uniform_u32(rt.count[e]) : 0;
         auto work = [&](auto nt, auto na) {
             constexpr int NT = decltype(nt)::value, RG = kUpRows * decltype(na)::value;
             using G = Gemv<DT, RG, NT, false>;
@@ -497,9 +536,9 @@ __global__ __launch_bounds__(kUpThreads) void k_moe_up_gemv(MoeArgs a, ExpertPtr
 
 // The second: a workgroup takes RG rows of hidden, its waves split the contraction over (expert, ffn).
 template <int DT, int RG, int TT, int W>
-__global__ __launch_bounds__(64 * W) void k_moe_down_gemv(MoeArgs a, ExpertPtrs ex, const Routing* in, const float* hbuf)
+__global__ __launch_bounds__(64 * W) void k_moe_down_gemv(MoeArgs a, ExpertPtrs ex, const Routing* in, const float* hbuf,
+                                                          float* parts, int splits)
 {
-    using T = typename Elem<DT>::T;
     __shared__ Routing rt;
     __shared__ float sums[W][TT][RG];
     __shared__ float red[W][RG * TT];
@@ -509,19 +548,20 @@ __global__ __launch_bounds__(64 * W) void k_moe_down_gemv(MoeArgs a, ExpertPtrs 
     if (lane < RG * TT)
         sums[wave][lane / RG][lane % RG] = 0.0f;
     __syncthreads();
-    const int64_t D = a.l.hidden, F = a.l.ffn, pitch = moe_pitch(F), d0 = (int64_t)blockIdx.x * RG;
-    const uint32_t reached = uniform_u32(rt.reached);
-    const int n = __popc(reached);
+    const int64_t D = a.l.hidden, F = a.l.ffn, pitch = moe_pitch(F);
+    const int grp = blockIdx.x / splits, split = blockIdx.x % splits;
+    const int64_t d0 = (int64_t)grp * RG;
+    const int me = split * W + wave, all = splits * W;
+    const int n = (int)uniform_u32(rt.units);
     constexpr int kRun = Gemv<DT, RG, TT, true>::kRun;
-    const int64_t runs = F / kRun, s0 = runs * n * wave / W, s1 = runs * n * (wave + 1) / W;
-    uint32_t left = reached;
-    for (int k = 0; k < n; ++k, left &= left - 1) {
+    const int64_t runs = (F + kRun - 1) / kRun, s0 = runs * n * me / all, s1 = runs * n * (me + 1) / all;
+    for (int k = 0; k < n; ++k) {
         const int64_t lo = s0 > runs * k ? s0 - runs * k : 0;
         const int64_t hi = s1 < runs * (k + 1) ? s1 - runs * k : runs;
-        const bool rest = F % kRun && k % W == wave;
-        if (lo >= hi && !rest)
+        if (lo >= hi)
             continue;
-        const int e = __ffs(left) - 1, c = (int)uniform_u32(rt.count[e]);
+        const Unit u = unit_of(rt, k);
+        const int e = u.e, c = u.n;
         auto work = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             using G = Gemv<DT, RG, NT, true>;
@@ -536,9 +576,7 @@ __global__ __launch_bounds__(64 * W) void k_moe_down_gemv(MoeArgs a, ExpertPtrs 
                     h_row(hbuf, a, rt, e, (int)uniform_u32(rt.list[e][t < c ? t : c - 1]), pitch));
             G g;
             g.clear();
-            g.runs(w, x, lo, 1, hi - lo);
-            if (rest)
-                g.rest(w, x, F);
+            g.runs(w, x, lo, 1, hi - lo, F);
             g.put(red[wave]);
             __builtin_amdgcn_wave_barrier();  // the wave's own LDS, in order
             if (lane < RG * NT && lane % NT < c)
@@ -554,88 +592,111 @@ __global__ __launch_bounds__(64 * W) void k_moe_down_gemv(MoeArgs a, ExpertPtrs 
                 work(std::integral_constant<int, 4>{});
     }
     __syncthreads();
-    const int tok = threadIdx.x / RG;
-    const int64_t d = d0 + threadIdx.x % RG;
-    if (tok >= a.T || d >= D)
-        return;
-    float y = 0.0f;
+    finish_rows<DT, RG>(a, d0, split, splits, parts, [&](int tok, int row) {
+        float y = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-        y += sums[w][tok][threadIdx.x % RG];
-    if (a.residual)
-        y += (float)static_cast<const T*>(a.residual)[tok * a.ldr + d];
-    static_cast<T*>(a.y)[tok * a.ldy + d] = (T)y;
+        for (int w = 0; w < W; ++w)
+            y += sums[w][tok][row];
+        return y;
+    });
 }
 
 // ---------------------------------------------------------------- which kernel
 // Waves that an item of the first kernel is split over: enough to fill the chip.
+constexpr int kUpGroups = 512;
 int up_split(int64_t items) { return items >= 4096 ? 1 : items >= 2048 ? 2 : items >= 1024 ? 4 : 8; }
 
 // Experts reached at most.
 int64_t most_experts(const MoeArgs& a) { return a.T * a.l.top_k < a.E ? a.T * a.l.top_k : a.E; }
 
-template <int WS>
-using int_c = std::integral_constant<int, WS>;
+// Workgroups per row group of the second kernel, with a KB of weight rows for
+// each of their waves.  Fewer than 128 row groups are split, into 256 workgroups
+// (20 tokens, 16 experts of 256 x 4000: 95 us with 16 workgroups, 46 with 256;
+// five tokens through eight of 1536 x 8960: 121 us with 96, 104 with 192).
+constexpr int kMaxSplit = 16;
+int down_split(const mp_moe_layer& l, int64_t most, int64_t groups, int waves)
+{
+    const int64_t want = groups < 128 ? 256 / groups : 1;
+    const int64_t room = most * l.ffn * (l.dtype == MP_F32 ? 4 : 2) / (1024 * waves);
+    const int64_t s = want < room ? want : room;
+    return (int)(s < 1 ? 1 : s > kMaxSplit ? kMaxSplit : s);
+}
+
+// The workspace: routing, h, the parts of a split second kernel.
+struct MoeWs {
+    Routing* rt;
+    char* h;
+    float* parts;
+    uint64_t bytes;
+};
+MoeWs moe_ws(const mp_moe_layer& l, int64_t tokens, void* ws)
+{
+    char* p = static_cast<char*>(ws);
+    const uint64_t h = 4ull * (uint64_t)tokens * (uint64_t)l.top_k * (uint64_t)moe_pitch(l.ffn);  // a plane of 4 bytes or two of 2
+    const uint64_t parts = l.hidden < 128 * 16 ? 4ull * kMaxSplit * (uint64_t)tokens * (uint64_t)l.hidden : 0;
+    return MoeWs{reinterpret_cast<Routing*>(p), p + sizeof(Routing), reinterpret_cast<float*>(p + sizeof(Routing) + h),
+                 sizeof(Routing) + h + parts};
+}
 
 template <typename F>
 void with_split(int ws, F go)
 {
     if (ws == 1)
-        go(int_c<1>{});
+        go(std::integral_constant<int, 1>{});
     else if (ws == 2)
-        go(int_c<2>{});
+        go(std::integral_constant<int, 2>{});
     else if (ws == 4)
-        go(int_c<4>{});
+        go(std::integral_constant<int, 4>{});
     else
-        go(int_c<8>{});
+        go(std::integral_constant<int, 8>{});
 }
 
-template <int DT, int TT>
+template <int DT>
+void join(const MoeArgs& a, const MoeWs& m, int splits, hipStream_t st)
+{
+    if (splits > 1)
+        hipLaunchKernelGGL(k_moe_join<DT>, dim3((unsigned)((a.T * a.l.hidden + 255) / 256)), dim3(256), 0, st, a,
+                           m.parts, splits);
+}
+
+template <int DT, int T8>
 hipError_t moe_tiles(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStream_t st)
 {
-    Routing* rt = static_cast<Routing*>(ws);
-    char* h = static_cast<char*>(ws) + sizeof(Routing);
+    const MoeWs m = moe_ws(a.l, a.T, ws);
     const int64_t items = (a.l.ffn + 15) / 16 * most_experts(a);
-    int split = up_split(items); int G1 = 512;
-    if (const char* ev = getenv("MOE_WS")) split = atoi(ev);
-    if (const char* ev = getenv("MOE_G1")) G1 = atoi(ev);
+    const int split = up_split(items);
     const int64_t need = (items * split + kUpWaves - 1) / kUpWaves;
     with_split(split, [&](auto s) {
-        hipLaunchKernelGGL((k_moe_up<DT, TT, decltype(s)::value>), dim3((unsigned)(need < G1 ? need : G1)),
-                           dim3(kUpThreads), 0, st, a, ex, rt, h);
+        hipLaunchKernelGGL((k_moe_up<DT, T8, decltype(s)::value>), dim3((unsigned)(need < kUpGroups ? need : kUpGroups)),
+                           dim3(kUpThreads), 0, st, a, ex, m.rt, m.h);
     });
-    const dim3 g2((unsigned)((a.l.hidden + 15) / 16));
-    int W2 = 16;
-    if (const char* ev = getenv("MOE_W2")) W2 = atoi(ev);
-    if (W2 == 16)
-    hipLaunchKernelGGL((k_moe_down<DT, TT, 16>), g2, dim3(1024), 0, st, a, ex, rt, h);
-    else
-    hipLaunchKernelGGL((k_moe_down<DT, TT, 8>), g2, dim3(512), 0, st, a, ex, rt, h);
+    const int64_t groups = (a.l.hidden + 15) / 16;
+    constexpr int W = 8;
+    const int splits = down_split(a.l, most_experts(a), groups, W);
+    hipLaunchKernelGGL((k_moe_down<DT, T8, W>), dim3((unsigned)(groups * splits)), dim3(64 * W), 0, st, a, ex, m.rt,
+                       m.h, m.parts, splits);
+    join<DT>(a, m, splits, st);
     return hipGetLastError();
 }
 
 template <int DT, int TT>
 hipError_t moe_gemv(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStream_t st)
 {
-    Routing* rt = static_cast<Routing*>(ws);
-    float* h = reinterpret_cast<float*>(static_cast<char*>(ws) + sizeof(Routing));
+    const MoeWs m = moe_ws(a.l, a.T, ws);
+    float* h = reinterpret_cast<float*>(m.h);
     const int64_t items = (a.l.ffn + kUpRows - 1) / kUpRows * most_experts(a);
-    int split = up_split(items); int G1 = 512;
-    if (const char* ev = getenv("MOE_WS")) split = atoi(ev);
-    if (const char* ev = getenv("MOE_G1")) G1 = atoi(ev);
+    const int split = up_split(items);
     const int64_t need = (items * split + kUpWaves - 1) / kUpWaves;
     with_split(split, [&](auto s) {
-        hipLaunchKernelGGL((k_moe_up_gemv<DT, TT, decltype(s)::value>), dim3((unsigned)(need < G1 ? need : G1)),
-                           dim3(kUpThreads), 0, st, a, ex, rt, h);
+        hipLaunchKernelGGL((k_moe_up_gemv<DT, TT, decltype(s)::value>), dim3((unsigned)(need < kUpGroups ? need : kUpGroups)),
+                           dim3(kUpThreads), 0, st, a, ex, m.rt, h);
     });
-    int W2 = 8;
-    if (const char* ev = getenv("MOE_W2")) W2 = atoi(ev);
-    constexpr int RG = 4;
-    const dim3 g2((unsigned)((a.l.hidden + RG - 1) / RG));
-    if (W2 == 8)
-    hipLaunchKernelGGL((k_moe_down_gemv<DT, RG, TT, 8>), g2, dim3(512), 0, st, a, ex, rt, h);
-    else
-    hipLaunchKernelGGL((k_moe_down_gemv<DT, RG, TT, 4>), g2, dim3(256), 0, st, a, ex, rt, h);
+    constexpr int RG = 4, W = 8;
+    const int64_t groups = (a.l.hidden + RG - 1) / RG;
+    const int splits = down_split(a.l, most_experts(a), groups, W);
+    hipLaunchKernelGGL((k_moe_down_gemv<DT, RG, TT, W>), dim3((unsigned)(groups * splits)), dim3(64 * W), 0, st, a, ex,
+                       m.rt, h, m.parts, splits);
+    join<DT>(a, m, splits, st);
     return hipGetLastError();
 }
 
@@ -646,9 +707,9 @@ hipError_t moe_d(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStream_t s
         return moe_gemv<DT, 1>(a, ex, ws, st);
     if (a.T <= kGemvTokens)
         return moe_gemv<DT, 4>(a, ex, ws, st);
-    if (a.T <= 16)
+    if (a.T <= 8)
         return moe_tiles<DT, 1>(a, ex, ws, st);
-    if (a.T <= 32)
+    if (a.T <= 16)
         return moe_tiles<DT, 2>(a, ex, ws, st);
     return moe_tiles<DT, 4>(a, ex, ws, st);
 }
@@ -662,8 +723,7 @@ hipError_t launch_moe(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStrea
 
 uint64_t moe_ws_bytes(const mp_moe_layer& l, int64_t tokens)
 {
-    // fp32: one plane of 4 bytes; bf16: two of 2
-    return sizeof(Routing) + 4ull * (uint64_t)tokens * (uint64_t)l.top_k * (uint64_t)moe_pitch(l.ffn);
+    return moe_ws(l, tokens, nullptr).bytes;
 }
 
 }  // namespace mp

@@ -1,19 +1,6 @@
-// Products of a weight matrix's rows with a few tokens on the matrix cores,
-// straight from memory: what mp_linear with few tokens and mp_moe share.
-//
-// The weights are read once and by one wave each, so they go from memory to
-// registers with no stop in LDS.  A step takes R = 16, 8 or 4 rows and G = 16 / R
-// pieces of 64 bytes of each, side by side.  Lane l holds the 16-byte chunk
-// l / 16 of piece (l % 16) / R of row (l % 16) % R, which is the A operand of a
-// 16 x 16 MFMA whose row p R + r is piece p of row r.  The tokens are the B
-// operand, one for each piece; a product with piece p's B operand is right
-// in the rows of piece p, which is one lane's 4 accumulators, so each piece has
-// accumulators of its own and a lane keeps those of piece (l / 16) * 4 / R: 4
-// outputs of token l % 16.  The order of the contraction inside a piece is
-// the operands' (bf16: one MFMA of depth 32; fp32: four of depth 4, the j-th
-// over element j of every chunk).  Fewer rows a step make more workgroups of
-// the same matrix and longer runs in memory, at G times the MFMAs and token
-// loads.
+// Products of a weight matrix's rows with a few tokens: what mp_linear with
+// few tokens and mp_moe share.  Few: up to 64 tokens on the matrix cores.  Gemv:
+// up to four on the vector ALU.
 #pragma once
 
 #include "ffn_common.h"
@@ -37,176 +24,168 @@ __device__ inline f32x4 mma16(const uint4& a, const uint4& b, f32x4 c)
     }
 }
 
-constexpr int kPieceBytes = 64;
-
-// A wave's operands: NA row tiles, TT token tiles of XS operands each.
-template <int DT, int R, int NA, int TT, int XS>
+// ---------------------------------------------------------------- up to 64 tokens
+// A wave multiplies NA tiles of 16 weight rows by the tokens, 128 bytes of every
+// row (a block) at a time.  Weights and tokens come from memory in whole lines,
+// 8 lanes to a row, into registers, and go through the wave's own LDS into the
+// operand layout, where neighbouring lanes hold neighbouring rows: loaded in
+// that layout, each of the 64 lanes' chunks is a cache access of its own, and
+// the cache takes one a cycle (3.2 TB/s of weights with two token loads per
+// weight load).  No barriers: a wave's LDS accesses are in order.  Weight rows
+// are the A operand, tokens the B operand: lane l then holds outputs 4 (l / 16)
+// .. + 3 of token l % 16.  The order of the contraction inside 64 bytes is the
+// operands' (bf16: one MFMA of depth 32; fp32: four of depth 4, the j-th over
+// element j of every chunk).  T8: tokens in eights (1, 2, 4 or 8).  With XS = 2
+// a token is the sum of two operands.
+template <int DT, int NA, int T8, int XS>
 struct Few {
-    static constexpr int G = 16 / R, XT = TT * XS, kStep = kPieceBytes * G, kElems = kStep / Fmt<DT>::esize;
-    const char* w[NA];  // the lane's chunk of step 0 in a row tile
-    const char* x[XT];  // its chunk of piece 0 of step 0 in a token tile: t, and with XS = 2 a second operand at TT + t
-    f32x4 acc[NA][TT][G];
+    static constexpr int V = Fmt<DT>::V, kElems = 128 / Fmt<DT>::esize, NT = (T8 + 1) / 2;
+    static constexpr int kLds = (NA * 16 + T8 * 8) * 128;  // bytes of LDS per wave
+    // blocks in flight: about 64 registers of them
+    static constexpr int kLoads = 2 * NA + XS * T8;
+    static constexpr int kRound = kLoads <= 4 ? 4 : kLoads <= 8 ? 2 : 1;
+    const char* w[NA][2];   // the lane's chunk of block 0 in rows row_of(lane, m)
+    const char* x[XS][T8];  // and of tokens row_of(lane, m)
+    char* lds;              // the wave's kLds bytes
+    f32x4 acc[NA][NT];
 
-    // Byte offset of the lane's chunk in a step, in a row's and in a token's.
-    __device__ static inline int row_of(int lane) { return (lane & 15) % R; }
-    __device__ static inline int w_off(int lane) { return (lane & 15) / R * kPieceBytes + (lane >> 4) * 16; }
-    __device__ static inline int x_off(int lane) { return (lane >> 4) * 16; }
+    struct Regs {
+        uint4 a[NA][2], b[XS][T8];
+    };
+    __device__ static inline int row_of(int lane, int m) { return m * 8 + (lane >> 3); }
+    __device__ static inline int off(int lane) { return (lane & 7) * 16; }
 
     __device__ inline void clear()
     {
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                    acc[i][t][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < NT; ++t)
+                acc[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-
-    // Loads of step `at` from the pointers, and the products with them.
-    struct Regs {
-        uint4 a[NA], b[XT][G];
-    };
-    __device__ static inline void load(Regs& r, const char* const (&wp)[NA], const char* const (&xp)[XT], int at)
+    // Block `at`.  PART: the row has `left` more elements, a block's or fewer; the rest reads as zeros.
+    template <bool PART>
+    __device__ inline void load(Regs& r, int64_t at, int left) const
     {
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-            r.a[i] = ld16u(wp[i] + at * kStep);
-#pragma unroll
-        for (int t = 0; t < XT; ++t)
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-                r.b[t][g] = ld16u(xp[t] + at * kStep + g * kPieceBytes);
-    }
-    __device__ inline void mul(const Regs& r)
-    {
-#pragma unroll
-        for (int t = 0; t < XT; ++t)
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-#pragma unroll
-                for (int i = 0; i < NA; ++i)
-                    acc[i][t % TT][g] = mma16<DT>(r.a[i], r.b[t][g], acc[i][t % TT][g]);
-            }
-    }
-
-    // Adds rounds [r0, r1) of kRound steps.  A round is in flight: each step is
-    // multiplied when it arrives and the same step of the next round takes its
-    // registers.  No load hangs on a branch: the compiler then knows how many
-    // are in flight and waits for the oldest alone (with a branch around the
-    // tokens' loads it waited for all of them once a round).  Lanes without a
-    // token therefore load another's.
-    static constexpr int kRound = NA + XT * G <= 3 ? 4 : 2;
-    __device__ inline void rounds(int64_t r0, int64_t r1)
-    {
-        if (r0 >= r1)
-            return;
-        const char *wp[NA], *xp[XT];
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-            wp[i] = w[i] + r0 * (kRound * kStep);
-#pragma unroll
-        for (int t = 0; t < XT; ++t)
-            xp[t] = x[t] + r0 * (kRound * kStep);
-        Regs r[kRound];
-#pragma unroll
-        for (int u = 0; u < kRound; ++u)
-            load(r[u], wp, xp, u);
-        for (int64_t k = r0 + 1; k < r1; ++k) {
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-                wp[i] += kRound * kStep;
-#pragma unroll
-            for (int t = 0; t < XT; ++t)
-                xp[t] += kRound * kStep;
-#pragma unroll
-            for (int u = 0; u < kRound; ++u) {
-                mul(r[u]);
-                __builtin_amdgcn_sched_barrier(0);  // or a step's loads move up and need registers of their own
-                load(r[u], wp, xp, u);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kRound; ++u)
-            mul(r[u]);
-    }
-
-    // What is left of a row of n elements behind its whole rounds: steps, and part of one.
-    __device__ inline void rest(int64_t n)
-    {
-        int64_t s = n / kElems / kRound * kRound;
-        const char *wp[NA], *xp[XT];
-        for (; s < n / kElems; ++s) {
-            Regs r;
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-                wp[i] = w[i] + s * kStep;
-#pragma unroll
-            for (int t = 0; t < XT; ++t)
-                xp[t] = x[t] + s * kStep;
-            load(r, wp, xp, 0);
-            mul(r);
-        }
-        if (n % kElems)
-            tail(s, (int)(n % kElems));
-    }
-    __device__ static inline int64_t whole(int64_t n) { return n / (kElems * kRound); }
-    __device__ static inline bool more(int64_t n) { return n % (kElems * kRound) != 0; }
-
-    // The n elements (fewer than a step holds) from step s on.
-    __device__ inline void tail(int64_t s, int n)
-    {
-        constexpr int V = Fmt<DT>::V;
-        const int lane = threadIdx.x & 63;
-        const int64_t at = s * kStep;
-        auto part = [&](const char* p, int left) {
-            return left >= V ? ld16u(p) : left > 0 ? ld16_head<DT>(p, left) : make_uint4(0, 0, 0, 0);
+        const int have = left - (int)(threadIdx.x & 7) * V;
+        auto get = [&](const char* p) {
+            if constexpr (PART)
+                return have >= V ? ld16u(p) : have > 0 ? ld16_head<DT>(p, have) : make_uint4(0, 0, 0, 0);
+            else
+                return ld16u(p);
         };
 #pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const uint4 a = part(w[i] + at, n - w_off(lane) / Fmt<DT>::esize);
+        for (int i = 0; i < NA; ++i)
 #pragma unroll
-            for (int t = 0; t < XT; ++t)
+            for (int m = 0; m < 2; ++m)
+                r.a[i][m] = get(w[i][m] + at * 128);
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const int off = g * kPieceBytes + x_off(lane);
-                    const uint4 b = part(x[t] + at + g * kPieceBytes, n - off / Fmt<DT>::esize);
-                    acc[i][t % TT][g] = mma16<DT>(a, b, acc[i][t % TT][g]);
+        for (int s = 0; s < XS; ++s)
+#pragma unroll
+            for (int m = 0; m < T8; ++m)
+                r.b[s][m] = get(x[s][m] + at * 128);
+    }
+    // Chunk c of row `row` in LDS, permuted so that 8 lanes meet 8 different chunks of 128 bytes both ways.
+    __device__ static inline int slot(int row, int c) { return row * 128 + ((c ^ (row & 7)) << 4); }
+    __device__ inline void mul(const Regs& r)
+    {
+        const int lane = threadIdx.x & 63, col = lane & 15, q = lane >> 4;
+        char* const lx = lds + NA * 16 * 128;
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+                *reinterpret_cast<uint4*>(lds + slot(i * 16 + row_of(lane, m), lane & 7)) = r.a[i][m];
+#pragma unroll
+        for (int s = 0; s < XS; ++s) {
+#pragma unroll
+            for (int m = 0; m < T8; ++m)
+                *reinterpret_cast<uint4*>(lx + slot(row_of(lane, m), lane & 7)) = r.b[s][m];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint4 a[NA];
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+                    a[i] = *reinterpret_cast<const uint4*>(lds + slot(i * 16 + col, h * 4 + q));
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {  // with 8 tokens, columns 8 to 15 repeat them
+                    const uint4 b = *reinterpret_cast<const uint4*>(lx + slot(T8 == 1 ? col & 7 : t * 16 + col, h * 4 + q));
+#pragma unroll
+                    for (int i = 0; i < NA; ++i)
+                        acc[i][t] = mma16<DT>(a[i], b, acc[i][t]);
                 }
+            }
+            __builtin_amdgcn_wave_barrier();
         }
     }
-
-    // The lane's outputs: those of its piece, to be added over the pieces (sum_tiles).
+    // Adds blocks [b0, b1) of a row of n elements; b0 is a multiple of kRound,
+    // b1 one too or past the row's last block.  A round of kRound blocks is in
+    // flight: each is multiplied when it arrives and the same block of the
+    // next round takes its registers.  No load hangs on a branch there: the
+    // compiler then knows how many are in flight and waits for the oldest
+    // alone.  What is left of a row behind its whole rounds is loaded at once.
+    __device__ inline void blocks(int64_t b0, int64_t b1, int64_t n)
+    {
+        const int64_t full = n / kElems / kRound;  // rounds without an end of the row
+        const int64_t r0 = b0 / kRound, r1 = b1 / kRound < full ? b1 / kRound : full;
+        Regs r[kRound];
+        if (r0 < r1) {
+#pragma unroll
+            for (int u = 0; u < kRound; ++u)
+                load<false>(r[u], r0 * kRound + u, 0);
+            for (int64_t k = r0 + 1; k < r1; ++k) {
+#pragma unroll
+                for (int u = 0; u < kRound; ++u) {
+                    mul(r[u]);
+                    __builtin_amdgcn_sched_barrier(0);  // or a block's loads move up and need registers of their own
+                    load<false>(r[u], k * kRound + u, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kRound; ++u)
+                mul(r[u]);
+        }
+        if (b1 > full * kRound && full * kRound * kElems < n) {
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) {
+                const int64_t left = n - (full * kRound + u) * kElems;
+                load<true>(r[u], full * kRound + u, (int)(left < 0 ? 0 : left < kElems ? left : kElems));
+            }
+#pragma unroll
+            for (int u = 0; u < kRound; ++u)
+                mul(r[u]);
+        }
+    }
+    // Share `part` of `parts` of a row of n elements.
+    __device__ inline void row(int64_t n, int part, int parts)
+    {
+        const int64_t rounds = (n + kElems * kRound - 1) / (kElems * kRound);
+        blocks(rounds * part / parts * kRound, rounds * (part + 1) / parts * kRound, n);
+    }
+    // The lane's 4 outputs of row tile i and token tile t.
     __device__ inline float4 out(int i, int t) const
     {
-        const int g = (threadIdx.x & 63) / 16 * 4 / R;
-        f32x4 v = acc[i][t][0];
-#pragma unroll
-        for (int k = 1; k < G; ++k)
-            v = g == k ? acc[i][t][k] : v;
-        return make_float4(v[0], v[1], v[2], v[3]);
+        return make_float4(acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3]);
     }
 };
 
-// Adds partial tiles over W waves and the pieces: red holds N tiles of 64
-// float4 per wave.  use(tile, row, token, sum): one output, spread over `n`
-// threads numbered `me`.  Callers put barriers around it.
-template <int R, int N, int W, typename F>
-__device__ inline void sum_tiles(const float4* red, int me, int n, F use)
+// Adds W waves' partial tiles: wave w's N tiles of 64 float4 are at red + w *
+// pitch.  use(tile, row, token, sum): one output, spread over `n` threads
+// numbered `me`.  Callers put barriers around it.
+template <int N, int W, typename F>
+__device__ inline void sum_tiles(const float4* red, int pitch, int me, int n, F use)
 {
-    constexpr int kOuts = R * 16;  // outputs of a tile
     const float* r = reinterpret_cast<const float*>(red);
-    for (int q = me; q < N * kOuts; q += n) {
-        const int tile = q / kOuts, o = q % kOuts;
-        // float4 o / 4 holds rows 4 (o / 64) .. + 3 of token o / 4 % 16
+    for (int q = me; q < N * 256; q += n) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w)
-#pragma unroll
-            for (int g = 0; g < 16 / R; ++g)
-                s += r[(w * N + tile) * 256 + g * kOuts + o];
-        use(tile, o / 64 * 4 + (o & 3), o / 4 % 16, s);
+            s += r[w * pitch * 4 + q];
+        // float4 o / 4 of a tile holds rows 4 (o / 64) .. + 3 of token o / 4 % 16
+        const int o = q % 256;
+        use(q / 256, o / 64 * 4 + (o & 3), o / 4 % 16, s);
     }
 }
 
@@ -256,11 +235,13 @@ struct Gemv {
                     acc[i][t] = fmaf(f[j], x[t][j], acc[i][t]);
         }
     }
-    // Runs c0, c0 + step, .. (n of them) of the rows w and the tokens x, which are the same for the wave.
+    // Runs c0, c0 + step, .. (cnt of them) of the rows w and the tokens x, which
+    // are the same for the wave; a row has n columns, and the run that ends it
+    // may be a part of one.
     __device__ inline void runs(const char* const (&w)[RG], const char* const (&x)[TT], int64_t c0, int64_t step,
-                                int64_t n)
+                                int64_t cnt, int64_t n)
     {
-        if (n <= 0)
+        if (cnt <= 0)
             return;
         const uint32_t lane = threadIdx.x & 63, wo = lane * 16, xo = lane * (V * kXs);
         auto load = [&](Regs& r, int64_t c) {
@@ -273,43 +254,43 @@ struct Gemv {
                 for (int k = 0; k < XC; ++k)
                     r.b[t][k] = ld16u(x[t] + c * (kRun * kXs) + k * 16 + xo);
         };
+        const bool part = (c0 + (cnt - 1) * step + 1) * kRun > n;
+        const int64_t full = part ? cnt - 1 : cnt;
         Regs cur, nxt;
-        load(cur, c0);
-        for (int64_t i = 1; i < n; ++i) {
+        if (full > 0)
+            load(cur, c0);
+        for (int64_t i = 1; i < full; ++i) {
             load(nxt, c0 + i * step);
             fma(cur);
             cur = nxt;
         }
-        fma(cur);
-    }
-    // The columns of a row of n behind its whole runs.
-    __device__ inline void rest(const char* const (&w)[RG], const char* const (&x)[TT], int64_t n)
-    {
-        const int64_t at = n / kRun * kRun + (threadIdx.x & 63) * V;
-        const int64_t left = n - at;
-        Regs r;
+        if (part) {
+            const int64_t at = n / kRun * kRun + lane * V, left = n - at;
 #pragma unroll
-        for (int i = 0; i < RG; ++i)
-            r.a[i] = left >= V ? ld16u(w[i] + at * es) : left > 0 ? ld16_head<DT>(w[i] + at * es, left) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < RG; ++i)
+                nxt.a[i] = left >= V ? ld16u(w[i] + at * es)
+                                     : left > 0 ? ld16_head<DT>(w[i] + at * es, left) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
+            for (int t = 0; t < TT; ++t)
 #pragma unroll
-            for (int k = 0; k < XC; ++k) {
-                constexpr int kPer = 16 / kXs;  // values of a 16-byte chunk
-                const int64_t l = left - k * kPer;
-                const char* p = x[t] + at * kXs + k * 16;
-                r.b[t][k] = l >= kPer ? ld16u(p)
-                                      : l > 0 ? ld16_head<XF ? MP_F32 : DT>(p, l) : make_uint4(0, 0, 0, 0);
-            }
-        fma(r);
+                for (int k = 0; k < XC; ++k) {
+                    constexpr int kPer = 16 / kXs;  // values of a 16-byte chunk
+                    const int64_t l = left - k * kPer;
+                    const char* p = x[t] + at * kXs + k * 16;
+                    nxt.b[t][k] = l >= kPer ? ld16u(p)
+                                            : l > 0 ? ld16_head<XF ? MP_F32 : DT>(p, l) : make_uint4(0, 0, 0, 0);
+                }
+        }
+        if (full > 0)
+            fma(cur);
+        if (part)
+            fma(nxt);
     }
     // All of a row of n, split over W waves.
     __device__ inline void row(const char* const (&w)[RG], const char* const (&x)[TT], int64_t n, int wave, int W)
     {
-        const int64_t c = n / kRun;
-        runs(w, x, wave, W, (c - wave + W - 1) / W);
-        if (wave == (int)(c % W) && n % kRun)
-            rest(w, x, n);
+        const int64_t c = (n + kRun - 1) / kRun;
+        runs(w, x, wave, W, (c - wave + W - 1) / W, n);
     }
     // The wave's sums, into red[RG][TT].
     __device__ inline void put(float* red)

@@ -303,8 +303,13 @@ uint64_t moe_ws_bytes(const mp_moe_layer& l, int64_t tokens);
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int hip_fail(hipError_t e, const char* what);
 void clear_error();
-// Device memory of at least `bytes` bytes from p on the current device.
-int check_device_buffer(const void* p, size_t bytes, const char* name);
+// Device memory of at least `bytes` bytes from p on the current device; *seen
+// (if given) receives the allocation it lies in, where the runtime tells.
+struct Allocation {
+    const char* p = nullptr;
+    size_t n = 0;
+};
+int check_device_buffer(const void* p, size_t bytes, const char* name, Allocation* seen = nullptr);
 int check_pinned_buffer(const void* p, size_t bytes, const char* name, const void** dev);
 
 // z with P(|Z| > z) = rho for a standard normal Z (0 unless 0 < rho < 1);
