@@ -58,6 +58,28 @@ __device__ inline uint4 ld16_head(const void* p, int64_t n)
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The chunk at p of which `have` elements count (any number; none if it is not
+// positive), zeros after them, without a branch: it is read from p, or, where
+// that passes the matrix's end, from `last`, its last 16 bytes, and shifted.
+template <int DT>
+__device__ inline uint4 ld16_edge(const char* p, int64_t have, const char* last)
+{
+    const char* q = p < last ? p : last;
+    const uint4 c = ld16u(q);
+    const uint64_t d = (uint64_t)(p - q);
+    const uint32_t sh = d < 15 ? (uint32_t)d * 8 : 120;  // bits
+    uint64_t lo = c.x | (uint64_t)c.y << 32, hi = c.z | (uint64_t)c.w << 32;
+    // (hi << 1) << (63 - n) is hi << (64 - n) for n from 0 on
+    const uint32_t n = sh & 63;
+    const uint64_t down = lo >> n | (hi << 1) << (63 - n);
+    lo = sh < 64 ? down : hi >> n;
+    hi = sh < 64 ? hi >> n : 0;
+    constexpr int kBits = 8 * Fmt<DT>::esize;
+    const int keep = have <= 0 ? 0 : have >= Fmt<DT>::V ? 128 : (int)have * kBits;  // bits
+    lo = keep >= 64 ? lo : lo & ((1ull << keep) - 1);
+    hi = keep >= 128 ? hi : keep <= 64 ? 0 : hi & ((1ull << (keep - 64)) - 1);
+    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
 template <int DT>
 __device__ inline void st16_head(void* p, uint4 c, int64_t n)
 {

@@ -34,8 +34,8 @@ struct Gemm {
     Epi epi;          // used by NT only
 };
 
-// ws: gemm_ws_bytes(dtype, form, I, J, P) bytes, 16-byte aligned.
+// ws: gemm_ws_bytes(dtype, I, J, P) bytes, 16-byte aligned.
 hipError_t launch_gemm(const Gemm& g, void* ws, hipStream_t st);
-uint64_t gemm_ws_bytes(int dtype, Form form, int64_t I, int64_t J, int64_t P);
+uint64_t gemm_ws_bytes(int dtype, int64_t I, int64_t J, int64_t P);
 
 }  // namespace mp

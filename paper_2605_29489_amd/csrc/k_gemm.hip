@@ -10,6 +10,8 @@ namespace {
 struct TileArgs {
     const char* a;
     const char* b;
+    const char* a_end;  // behind the operands' last elements
+    const char* b_end;
     void* c;
     int64_t lda, ldb, ldc;
     int64_t I, J, P;
@@ -32,6 +34,10 @@ struct Tile {
     static constexpr int FI = BM / 32, FJ = 4;                     // 16 x 16 pieces of a wave's BM/2 x 64
     static constexpr int kBufA = BM * kRowBytes, kBufB = BN * kRowBytes;
     static constexpr int LA = BM * 8 / kThreads, LB = BN * 8 / kThreads;  // 16-byte chunks per thread
+    // K tiles on their way in registers.  One in a 256 x 256 tile, whose K tile
+    // takes as long as a trip to memory; where few, small tiles share the chip
+    // the trip is what a K tile costs (1.1 us with one set, 128 x 128)
+    static constexpr int SETS = BM == 256 ? 1 : BM == 128 ? 2 : 4, UNROLL = SETS < 2 ? 2 : SETS;
 };
 
 // Byte offset of a chunk in an operand's LDS tile.  Rows of p side by side: 8
@@ -56,20 +62,23 @@ __device__ inline int lds_col(int k, int c)
 __device__ inline const char* at32(const char* base, uint32_t off) { return base + off; }
 
 // One operand's part of loading a K tile: which chunks a thread takes, global
-// memory to registers, registers to LDS.  Rows (columns of p-rows) past the
-// last repeat it or read as zeros; only p past the end has to be zero, for
-// both operands.
-template <int DT, int B, int N, int kThreads, bool ROWS, bool PERM>
+// memory to registers, registers to LDS.  Rows past the last repeat it, columns
+// of p-rows past the last are whatever follows them: their outputs are
+// dropped.  Only p past the end has to be zero, for both operands, and only the
+// matrix's end must not be passed: both concern the last K tile alone.
+template <int DT, int B, int N, int kThreads, bool ROWS, bool PERM, int SETS>
 struct Loader {
     static constexpr int es = Fmt<DT>::esize, V = Fmt<DT>::V, BK = kRowBytes / es, CPR = B * es / 16;
     const char* base;   // of the tile's first element at p = 0
+    const char* last;   // the matrix's last 16 bytes
     int64_t step;       // bytes from one K tile to the next
     uint32_t off[N];
-    int64_t cols;       // ROWS: columns left from the tile's first
-    uint4 r[N];
+    uint4 r[SETS][N];
 
-    __device__ inline void init(const char* p, int64_t ld, int64_t first, int64_t count)
+    // p: the operand at the part's first p; first, count: the tile's first row (column) and how many there are
+    __device__ inline void init(const char* p, int64_t ld, int64_t first, int64_t count, const char* end)
     {
+        last = end - 16;
         if constexpr (!ROWS) {
             base = p + first * ld * es;
             step = kRowBytes;
@@ -82,43 +91,43 @@ struct Loader {
         } else {
             base = p + first * es;
             step = ld * BK * es;
-            cols = count - first;
+            const int chunks = (int)((count - first + V - 1) / V < CPR ? (count - first + V - 1) / V : CPR);
 #pragma unroll
             for (int t = 0; t < N; ++t) {
-                const int idx = t * kThreads + threadIdx.x;
-                off[t] = (uint32_t)((idx / CPR) * ld * es) + (idx % CPR) * 16;
+                const int idx = t * kThreads + threadIdx.x, c = idx % CPR;
+                off[t] = (uint32_t)((idx / CPR) * ld * es) + (c < chunks ? c : chunks - 1) * 16;
             }
         }
     }
-    // K tile kt; left: elements of p from its first on
-    __device__ inline void load(int64_t kt, int64_t left)
+    // K tile kt, not the matrix's last, into register set `set`
+    __device__ inline void load(int set, int64_t kt)
     {
         const char* p = base + kt * step;
-        if (left >= BK && (!ROWS || cols >= B)) {
 #pragma unroll
-            for (int t = 0; t < N; ++t)
-                r[t] = ld16u(at32(p, off[t]));
-            return;
+        for (int t = 0; t < N; ++t) {
+            // as a value that may have changed, the offset stays 32 bits wide and
+            // goes into the load; else it is kept as 64 bits, in two registers
+            asm volatile("" : "+v"(off[t]));
+            r[set][t] = ld16u(at32(p, off[t]));
         }
+    }
+    // the last one, of which p has `left` elements
+    __device__ inline void load_last(int set, int64_t kt, int64_t left)
+    {
+        const char* p = base + kt * step;
 #pragma unroll
         for (int t = 0; t < N; ++t) {
             const int idx = t * kThreads + threadIdx.x;
-            int64_t have;
-            if constexpr (!ROWS)
-                have = left - (idx & 7) * V;
-            else
-                have = idx / CPR < left ? cols - (idx % CPR) * V : 0;
-            r[t] = have >= V ? ld16u(at32(p, off[t]))
-                             : have > 0 ? ld16_head<DT>(at32(p, off[t]), have) : make_uint4(0, 0, 0, 0);
+            r[set][t] = ld16_edge<DT>(at32(p, off[t]), ROWS ? (idx / CPR < left ? V : 0) : left - (idx & 7) * V, last);
         }
     }
-    __device__ inline void store(char* lds) const
+    __device__ inline void store(int set, char* lds) const
     {
 #pragma unroll
         for (int t = 0; t < N; ++t) {
             const int idx = t * kThreads + threadIdx.x;
             const int o = ROWS ? lds_col<DT, CPR>(idx / CPR, idx % CPR) : lds_row(idx >> 3, idx & 7, PERM);
-            *reinterpret_cast<uint4*>(lds + o) = r[t];
+            *reinterpret_cast<uint4*>(lds + o) = r[set][t];
         }
     }
 };
@@ -234,10 +243,10 @@ __device__ inline void which_tile(int id, int n, int ti, int tj, int* i, int* j)
 }
 
 template <int DT, Form F, int BM, int BN, int EPI>
-__global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads)) void k_gemm(TileArgs g)
+__global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads), BM == 64 ? 1 : 2) void k_gemm(TileArgs g)
 {
     using C = Tile<DT, F, BM, BN>;
-    constexpr bool PERM = !C::BR;
+    constexpr bool PERM = !C::BR, kPong = BM == 256;
     __shared__ __attribute__((aligned(16))) char lds[2 * (C::kBufA + C::kBufB)];
     int bi, bj;
     const int tiles = g.ti * g.tj, split = blockIdx.x / tiles;
@@ -249,10 +258,10 @@ __global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads)) void k_gemm(TileAr
     const int64_t pn = g.P - p0 < (int64_t)g.k_tiles * C::BK ? g.P - p0 : (int64_t)g.k_tiles * C::BK;
     const int nk = (int)((pn + C::BK - 1) / C::BK);
 
-    Loader<DT, BM, C::LA, C::kThreads, C::AR, false> la;
-    Loader<DT, BN, C::LB, C::kThreads, C::BR, PERM> lb;
-    la.init(g.a + p0 * C::es * (C::AR ? g.lda : 1), g.lda, i0, g.I);
-    lb.init(g.b + p0 * C::es * (C::BR ? g.ldb : 1), g.ldb, j0, g.J);
+    Loader<DT, BM, C::LA, C::kThreads, C::AR, false, C::SETS> la;
+    Loader<DT, BN, C::LB, C::kThreads, C::BR, PERM, C::SETS> lb;
+    la.init(g.a + p0 * C::es * (C::AR ? g.lda : 1), g.lda, i0, g.I, g.a_end);
+    lb.init(g.b + p0 * C::es * (C::BR ? g.ldb : 1), g.ldb, j0, g.J, g.b_end);
 
     f32x4 acc[C::FI][C::FJ];
 #pragma unroll
@@ -277,36 +286,103 @@ __global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads)) void k_gemm(TileAr
                 acc[f][h] = mma16<DT>(b[h], a, acc[f][h]);
         }
     };
-    // K tile kt is multiplied from one buffer while tile kt + 1 goes from
-    // registers to the other and tile kt + 2 from memory to registers.
-    auto turn = [&](int kt, int buf) {
+    // The matrix's last K tile, which alone has edges, comes behind the loop
+    // over the tiles below `end`.  There, loads past them repeat the last one,
+    // so that no load hangs on a branch: the compiler then counts those in
+    // flight and waits for the oldest set alone.
+    const int end = split == g.splits - 1 ? nk - 1 : nk;
+    auto next = [&](int kt) { return kt < end ? kt : end - 1; };
+    // K tile kt is multiplied from one buffer while tile kt + 1 goes from its
+    // register set to the other and tile kt + 1 + SETS from memory to that set.
+    [[maybe_unused]] auto turn = [&](int kt, int buf, int set) {
         half(buf, 0);
-        if (kt + 1 < nk) {
-            la.store(sa + (buf ^ 1) * C::kBufA);
-            lb.store(sb + (buf ^ 1) * C::kBufB);
-            if (kt + 2 < nk) {
-                la.load(kt + 2, pn - (int64_t)(kt + 2) * C::BK);
-                lb.load(kt + 2, pn - (int64_t)(kt + 2) * C::BK);
-            }
-        }
+        la.store(set, sa + (buf ^ 1) * C::kBufA);
+        lb.store(set, sb + (buf ^ 1) * C::kBufB);
+        la.load(set, next(kt + 1 + C::SETS));
+        lb.load(set, next(kt + 1 + C::SETS));
         half(buf, 1);
         __syncthreads();
     };
-    if (nk > 0) {
-        la.load(0, pn);
-        lb.load(0, pn);
-        la.store(sa);
-        lb.store(sb);
-        if (nk > 1) {
-            la.load(1, pn - C::BK);
-            lb.load(1, pn - C::BK);
+    // The same with the two waves of a SIMD half a turn apart: while one reads
+    // its operands from LDS (and moves its part of the next tiles along), the
+    // other multiplies, and at the barrier they change over.  Without it the
+    // LDS and the matrix cores, each busy 2048 cycles a K tile, took turns.  A
+    // buffer is written while neither group reads it: the slower group's last
+    // reads of it are a barrier behind the faster one's first write, and the
+    // slower one's last write a barrier ahead of the faster one's first read.
+    [[maybe_unused]] auto step = [&](int kt, int buf, int ks) {
+        uint4 a[C::FI], b[C::FJ];
+#pragma unroll
+        for (int h = 0; h < C::FJ; ++h)
+            b[h] = piece<DT, BN, C::BR, PERM>(sb + buf * C::kBufB, wj, h, ks);
+#pragma unroll
+        for (int f = 0; f < C::FI; ++f)
+            a[f] = piece<DT, BM, C::AR, false>(sa + buf * C::kBufA, wi, f, ks);
+        if (ks == 0) {
+            la.store(0, sa + (buf ^ 1) * C::kBufA);
+            la.load(0, next(kt + 2));
+        } else {
+            lb.store(0, sb + (buf ^ 1) * C::kBufB);
+            lb.load(0, next(kt + 2));
         }
         __syncthreads();
-        for (int kt = 0; kt < nk; kt += 2) {
-            turn(kt, 0);
-            if (kt + 1 < nk)
-                turn(kt + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int f = 0; f < C::FI; ++f)
+#pragma unroll
+            for (int h = 0; h < C::FJ; ++h)
+                acc[f][h] = mma16<DT>(b[h], a[f], acc[f][h]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+    };
+    if (end > 0) {
+#pragma unroll
+        for (int u = 0; u < C::SETS; ++u) {
+            la.load(u, next(u));
+            lb.load(u, next(u));
         }
+        la.store(0, sa);
+        lb.store(0, sb);
+        la.load(0, next(C::SETS));
+        lb.load(0, next(C::SETS));
+        __syncthreads();
+        int kt = 0;
+        if constexpr (kPong) {
+            if (wave >= C::kThreads / 128)
+                __syncthreads();
+            for (; kt + 1 < end; kt += 2) {
+                step(kt, 0, 0);
+                step(kt, 0, 1);
+                step(kt + 1, 1, 0);
+                step(kt + 1, 1, 1);
+            }
+            if (kt < end) {
+                step(kt, 0, 0);
+                step(kt, 0, 1);
+            }
+            if (wave < C::kThreads / 128)
+                __syncthreads();
+        } else {
+            for (; kt + C::UNROLL <= end; kt += C::UNROLL)
+#pragma unroll
+                for (int u = 0; u < C::UNROLL; ++u)
+                    turn(kt + u, u & 1, (u + 1) % C::SETS);
+#pragma unroll
+            for (int u = 0; u < C::UNROLL - 1; ++u)
+                if (kt + u < end)
+                    turn(kt + u, u & 1, (u + 1) % C::SETS);
+        }
+    }
+    if (end < nk) {
+        la.load_last(0, end, pn - (int64_t)end * C::BK);
+        lb.load_last(0, end, pn - (int64_t)end * C::BK);
+        la.store(0, sa);
+        lb.store(0, sb);
+        __syncthreads();
+        half(0, 0);
+        half(0, 1);
     }
 
     // lane: row i0 + wi + f * 16 + lane % 16, and with PERM 16 adjacent columns
@@ -372,13 +448,20 @@ __global__ __launch_bounds__(256) void k_gemm_join(const float* part, int splits
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n; q += (int64_t)gridDim.x * 256) {
         const int64_t i = q / per, j = (q - i * per) * 4;
         const float* p = part + i * pitch + j;
-        float4 s = *reinterpret_cast<const float4*>(p);
-        for (int k = 1; k < splits; ++k) {
-            const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)k * I * pitch);
-            s.x += v.x;
-            s.y += v.y;
-            s.z += v.z;
-            s.w += v.w;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k0 = 0; k0 < splits; k0 += 4) {  // four loads at once
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[u] = k0 + u < splits ? *reinterpret_cast<const float4*>(p + (int64_t)(k0 + u) * I * pitch)
+                                       : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                s.x += v[u].x;
+                s.y += v[u].y;
+                s.z += v[u].z;
+                s.w += v[u].w;
+            }
         }
         float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
@@ -398,10 +481,11 @@ __global__ __launch_bounds__(256) void k_gemm_join(const float* part, int splits
     }
 }
 
-// Rows so far apart that the offsets inside a tile pass 32 bits: a 64 x 64 tile
+// Rows so far apart that the offsets inside a tile pass 32 bits, and operands of
+// a few bytes: a 64 x 64 tile
 // per workgroup on the vector ALU, 16 steps of p at a time, any strides.
 template <int DT>
-__global__ __launch_bounds__(256) void k_gemm_far(const typename Elem<DT>::T* a, int64_t ai, int64_t ap,
+__global__ __launch_bounds__(256) void k_gemm_any(const typename Elem<DT>::T* a, int64_t ai, int64_t ap,
                                                   const typename Elem<DT>::T* b, int64_t bj, int64_t bp, void* c,
                                                   int64_t ldc, int64_t I, int64_t J, int64_t P, int tj, Epi e)
 {
@@ -445,41 +529,57 @@ __global__ __launch_bounds__(256) void k_gemm_far(const typename Elem<DT>::T* a,
 
 // ---------------------------------------------------------------- which kernel
 struct Choice {
-    int big;      // 256 x 256 tiles, else 128 x 128
+    int tile;     // 256, 128 or 64
     int splits, k_tiles;
     int64_t ti, tj, pitch;
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-Choice choose(int dtype, Form form, int64_t I, int64_t J, int64_t P)
+// Tiles of 256 (bf16) where they give half the CUs one, of 128 where they give
+// every CU one, else of 64, with p split into parts of 16 K tiles and more
+// until there are 512 workgroups: the sum of the parts is a launch and 5 us.
+// us at one layer of m x n x k in bf16, by tile (parts):
+//   2048 4096 4096: 75 (256), 77 (128), 115 (64)
+//   1024 4096 4096: 114 (256), 46 (128), 59 (64)
+//    512 4096 4096: 43 (128), 36 (128, 2), 29 (64), 45 (64, 2)
+//    128 1536 8960: 88 (128), 44 (64), 19 (64, 8)
+//    300 1000  700: 15 (128), 10.5 (64), 11.8 (64, 2)
+Choice choose(int dtype, int64_t I, int64_t J, int64_t P)
 {
-    const int BK = dtype == MP_F32 ? 32 : 64;
-    const int64_t nk = ceil_div(P, BK);
+    const int BK = kRowBytes / (dtype == MP_F32 ? 4 : 2);
+    const int64_t nk = P > 0 ? ceil_div(P, BK) : 1;
     Choice c{};
-    c.big = dtype == MP_BF16 && ceil_div(I, 256) * ceil_div(J, 256) >= 160;
-    const int B = c.big ? 256 : 128;
-    c.ti = ceil_div(I, B);
-    c.tj = ceil_div(J, B);
-    // 128 x 128 tiles that leave CUs without work split p, 8 K tiles a part at least
+    c.tile = dtype == MP_BF16 && ceil_div(I, 256) * ceil_div(J, 256) >= 128 ? 256
+             : ceil_div(I, 128) * ceil_div(J, 128) >= 256                  ? 128
+                                                                           : 64;
+    c.ti = ceil_div(I, c.tile);
+    c.tj = ceil_div(J, c.tile);
     int64_t s = 1;
-    if (!c.big && c.ti * c.tj < 384) {
-        s = ceil_div(512, c.ti * c.tj);
-        const int64_t most = nk / 8;
-        s = s < most ? s : most;
+    if (c.tile == 64) {
+        const int64_t want = 512 / (c.ti * c.tj), most = nk / 16;
+        s = want < most ? want : most;
         s = s > 1 ? s : 1;
     }
-    c.k_tiles = (int)ceil_div(nk > 0 ? nk : 1, s);
-    c.splits = (int)ceil_div(nk > 0 ? nk : 1, c.k_tiles);
+    c.k_tiles = (int)ceil_div(nk, s);
+    c.splits = (int)ceil_div(nk, c.k_tiles);
     c.pitch = (J + 3) / 4 * 4;
     return c;
 }
 
-// Offsets inside a tile are 32 bits wide.
-bool far_apart(const Gemm& g)
+// Bytes from an operand's first element to behind its last.
+int64_t span(const Gemm& g, bool a)
+{
+    const bool rows = a ? g.form == Form::TN : g.form != Form::NT;  // its rows are p
+    const int64_t free = a ? g.I : g.J, n = rows ? g.P : free, cols = rows ? free : g.P;
+    return n == 0 || cols == 0 ? 0 : ((n - 1) * (a ? g.lda : g.ldb) + cols) * (g.dtype == MP_F32 ? 4 : 2);
+}
+
+// The tiled kernel takes 32-bit offsets inside a tile, and operands of 16 bytes at least.
+bool untiled(const Gemm& g)
 {
     const int64_t lim = (int64_t)1 << 31, es = g.dtype == MP_F32 ? 4 : 2;
-    return g.lda * es * 256 >= lim || g.ldb * es * 256 >= lim;
+    return g.lda * es * 256 >= lim || g.ldb * es * 256 >= lim || span(g, true) < 16 || span(g, false) < 16;
 }
 
 template <int DT, Form F, int B, int EPI>
@@ -493,20 +593,38 @@ void tile_go(const TileArgs& t, hipStream_t st)
 template <int DT, Form F>
 hipError_t gemm_go(const Gemm& g, const Choice& c, void* ws, hipStream_t st)
 {
-    TileArgs t{(const char*)g.a, (const char*)g.b, g.c,    g.lda,    g.ldb,     g.ldc,   g.I,  g.J,
-               g.P,              (int)c.ti,        (int)c.tj, c.splits, c.k_tiles, c.pitch, g.epi};
+    const char *a = (const char*)g.a, *b = (const char*)g.b;
+    TileArgs t{a,
+               b,
+               a + span(g, true),
+               b + span(g, false),
+               g.c,
+               g.lda,
+               g.ldb,
+               g.ldc,
+               g.I,
+               g.J,
+               g.P,
+               (int)c.ti,
+               (int)c.tj,
+               c.splits,
+               c.k_tiles,
+               c.pitch,
+               g.epi};
     constexpr int kEpi = F == Form::NT ? EPI_FULL : EPI_STORE;
     if (c.splits > 1) {
         t.c = ws;
-        tile_go<DT, F, 128, EPI_PART>(t, st);
+        tile_go<DT, F, 64, EPI_PART>(t, st);
         const int64_t n = ceil_div(g.I * c.pitch / 4, 256);
         hipLaunchKernelGGL(k_gemm_join<DT>, dim3((unsigned)(n < 4096 ? n : 4096)), dim3(256), 0, st, (const float*)ws,
                            c.splits, c.pitch, g.c, g.ldc, g.I, g.J, g.epi);
-    } else if (c.big) {
+    } else if (c.tile == 256) {
         if constexpr (DT == MP_BF16)
             tile_go<DT, F, 256, kEpi>(t, st);
-    } else {
+    } else if (c.tile == 128) {
         tile_go<DT, F, 128, kEpi>(t, st);
+    } else {
+        tile_go<DT, F, 64, kEpi>(t, st);
     }
     return hipGetLastError();
 }
@@ -515,15 +633,15 @@ template <int DT>
 hipError_t gemm_d(const Gemm& g, void* ws, hipStream_t st)
 {
     using T = typename Elem<DT>::T;
-    if (far_apart(g)) {
+    if (untiled(g)) {
         const bool ar = g.form == Form::TN, br = g.form != Form::NT;
         const int64_t ti = ceil_div(g.I, 64), tj = ceil_div(g.J, 64);
-        hipLaunchKernelGGL(k_gemm_far<DT>, dim3((unsigned)(ti * tj)), dim3(256), 0, st, (const T*)g.a,
+        hipLaunchKernelGGL(k_gemm_any<DT>, dim3((unsigned)(ti * tj)), dim3(256), 0, st, (const T*)g.a,
                            ar ? 1 : g.lda, ar ? g.lda : 1, (const T*)g.b, br ? 1 : g.ldb, br ? g.ldb : 1, g.c, g.ldc,
                            g.I, g.J, g.P, (int)tj, g.epi);
         return hipGetLastError();
     }
-    const Choice c = choose(DT, g.form, g.I, g.J, g.P);
+    const Choice c = choose(DT, g.I, g.J, g.P);
     switch (g.form) {
         case Form::NT: return gemm_go<DT, Form::NT>(g, c, ws, st);
         case Form::NN: return gemm_go<DT, Form::NN>(g, c, ws, st);
@@ -538,9 +656,9 @@ hipError_t launch_gemm(const Gemm& g, void* ws, hipStream_t st)
     return g.dtype == MP_F32 ? gemm_d<MP_F32>(g, ws, st) : gemm_d<MP_BF16>(g, ws, st);
 }
 
-uint64_t gemm_ws_bytes(int dtype, Form form, int64_t I, int64_t J, int64_t P)
+uint64_t gemm_ws_bytes(int dtype, int64_t I, int64_t J, int64_t P)
 {
-    const Choice c = choose(dtype, form, I, J, P);
+    const Choice c = choose(dtype, I, J, P);
     return c.splits > 1 ? 4ull * (uint64_t)c.splits * (uint64_t)I * (uint64_t)c.pitch : 0;
 }
 

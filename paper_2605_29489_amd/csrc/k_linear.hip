@@ -233,11 +233,11 @@ __global__ __launch_bounds__(256) void k_dz(const typename Elem<DT>::T* dy, int6
     }
 }
 
-// Bands of k_dz: enough workgroups to fill the chip, 8 rows a thread at least.
+// Bands of k_dz: enough workgroups to fill the chip, 2 rows a thread at least.
 int dz_bands(const mp_linear_shape& s)
 {
     const int V = s.dtype == MP_F32 ? 4 : 8;
-    const int64_t across = (s.n + 64 * V - 1) / (64 * V), want = (2048 + across - 1) / across, most = (s.m + 31) / 32;
+    const int64_t across = (s.n + 64 * V - 1) / (64 * V), want = (2048 + across - 1) / across, most = (s.m + 7) / 8;
     const int64_t n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 512 ? 512 : n);
 }
@@ -258,8 +258,8 @@ BackWs back_ws(const mp_linear_shape& s)
     w.gemm = w.part + (uint64_t)dz_bands(s) * (uint64_t)w.lddz * 4;
     uint64_t g = 0;
     if (s.m > 0 && s.n > 0 && s.k > 0) {
-        const uint64_t a = gemm_ws_bytes(s.dtype, Form::NN, s.m, s.k, s.n);
-        const uint64_t b = gemm_ws_bytes(s.dtype, Form::TN, s.n, s.k, s.m);
+        const uint64_t a = gemm_ws_bytes(s.dtype, s.m, s.k, s.n);
+        const uint64_t b = gemm_ws_bytes(s.dtype, s.n, s.k, s.m);
         g = a > b ? a : b;
     }
     w.bytes = w.gemm + g;
@@ -302,7 +302,7 @@ uint64_t linear_ws_bytes(const mp_linear_shape& s)
 {
     if (s.m <= kFewTokens || s.n == 0)
         return 0;
-    return gemm_ws_bytes(s.dtype, Form::NT, s.m, s.n, s.k);
+    return gemm_ws_bytes(s.dtype, s.m, s.n, s.k);
 }
 
 hipError_t launch_linear_backward(const mp_linear_shape& s, const void* dy, const void* x, const void* w,
