@@ -405,7 +405,8 @@ int mp_lora_merge_ties_tau(const mp_layout* layout, const void* base, const mp_l
  * MP_E_ARG: a null, misaligned, non-device or too small buffer, a size, ld,
  * flag or code out of range, or an output that overlaps another buffer of
  * the call (beyond what is allowed below); MP_E_HIP: the launch failed.
- * Sizes are at most 2^31 - 1 each, ld at most 2^40. */
+ * Sizes are at most 2^26 each (rows of a norm 2^31 - 1, hidden and ffn of a
+ * layer of experts 2^24), ld at most 2^40. */
 typedef enum {
     MP_ACT_NONE = 0,
     MP_ACT_RELU = 1,

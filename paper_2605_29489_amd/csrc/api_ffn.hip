@@ -10,9 +10,12 @@
 namespace mp {
 namespace {
 
-constexpr int64_t kMaxSize = 0x7fffffff, kMaxLd = (int64_t)1 << 40;
+// A launch takes fewer than 2^32 threads along x: up to kMaxSize rows or
+// columns of an operand, the kernels' grids stay below that.
+constexpr int64_t kMaxRows = 0x7fffffff, kMaxSize = (int64_t)1 << 26, kMaxHidden = (int64_t)1 << 24;
+constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
-// Bytes from a matrix's first element to its last: (rows - 1) * ld + cols elements.
+// A buffer of a call: n bytes from p on.
 struct Span {
     const char* p = nullptr;
     size_t n = 0;
@@ -20,9 +23,14 @@ struct Span {
     const char* name = "";
 };
 
+// Bytes from a matrix's first element to behind its last, (rows - 1) * ld +
+// cols elements; 2^62, more than any buffer holds, where that is beyond it.
 size_t span_bytes(int64_t rows, int64_t cols, int64_t ld, int es)
 {
-    return rows == 0 || cols == 0 ? 0 : ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * (size_t)es;
+    if (rows == 0 || cols == 0)
+        return 0;
+    const unsigned __int128 n = ((unsigned __int128)(rows - 1) * (uint64_t)ld + (uint64_t)cols) * (uint32_t)es;
+    return n >> 62 ? (size_t)1 << 62 : (size_t)n;
 }
 
 int check_dtype(int32_t dtype, int* es)
@@ -33,10 +41,10 @@ int check_dtype(int32_t dtype, int* es)
     return MP_OK;
 }
 
-int check_size(int64_t v, int64_t lo, const char* name)
+int check_size(int64_t v, int64_t lo, int64_t hi, const char* name)
 {
-    if (v < lo || v > kMaxSize)
-        return fail(MP_E_ARG, "%s = %lld must be in [%lld, 2^31)", name, (long long)v, (long long)lo);
+    if (v < lo || v > hi)
+        return fail(MP_E_ARG, "%s = %lld must be in [%lld, %lld]", name, (long long)v, (long long)lo, (long long)hi);
     return MP_OK;
 }
 
@@ -109,8 +117,8 @@ int check_linear_shape(const mp_linear_shape* s, int* es)
     if (s == nullptr)
         return fail(MP_E_ARG, "shape is NULL");
     int rc;
-    if ((rc = check_dtype(s->dtype, es)) || (rc = check_size(s->m, 0, "m")) || (rc = check_size(s->n, 0, "n")) ||
-        (rc = check_size(s->k, 0, "k")))
+    if ((rc = check_dtype(s->dtype, es)) || (rc = check_size(s->m, 0, kMaxSize, "m")) ||
+        (rc = check_size(s->n, 0, kMaxSize, "n")) || (rc = check_size(s->k, 0, kMaxSize, "k")))
         return rc;
     if (s->act < MP_ACT_NONE || s->act > MP_ACT_SILU)
         return fail(MP_E_ARG, "act %d is not an mp_act", s->act);
@@ -122,8 +130,8 @@ int check_norm_shape(const mp_norm_shape* s, int* es)
     if (s == nullptr)
         return fail(MP_E_ARG, "shape is NULL");
     int rc;
-    if ((rc = check_dtype(s->dtype, es)) || (rc = check_size(s->rows, 0, "rows")) ||
-        (rc = check_size(s->cols, 0, "cols")))
+    if ((rc = check_dtype(s->dtype, es)) || (rc = check_size(s->rows, 0, kMaxRows, "rows")) ||
+        (rc = check_size(s->cols, 0, kMaxSize, "cols")))
         return rc;
     if (s->flags & ~(int32_t)MP_NORM_RMS)
         return fail(MP_E_ARG, "flags %d: unknown bits", s->flags);
@@ -137,8 +145,8 @@ int check_moe_layer(const mp_moe_layer* l, int64_t tokens, int* es)
     if (l == nullptr)
         return fail(MP_E_ARG, "layer is NULL");
     int rc;
-    if ((rc = check_dtype(l->dtype, es)) || (rc = check_size(l->hidden, 1, "hidden")) ||
-        (rc = check_size(l->ffn, 1, "ffn")) || (rc = check_size(tokens, 0, "tokens")))
+    if ((rc = check_dtype(l->dtype, es)) || (rc = check_size(l->hidden, 1, kMaxHidden, "hidden")) ||
+        (rc = check_size(l->ffn, 1, kMaxHidden, "ffn")) || (rc = check_size(tokens, 0, kMaxRows, "tokens")))
         return rc;
     if (l->act < MP_ACT_NONE || l->act > MP_ACT_SILU)
         return fail(MP_E_ARG, "act %d is not an mp_act", l->act);
@@ -378,11 +386,9 @@ int mp_moe(const mp_moe_layer* layer, int64_t tokens, const void* x, int64_t ldx
         (ids && (rc = check_matrix(seen, ids, tokens, l.top_k, l.top_k, 4, "ids", &I))) ||
         (gates && (rc = check_matrix(seen, gates, tokens, l.top_k, l.top_k, 4, "gates", &G))))
         return rc;
-    const int64_t df = l.hidden * l.ffn;  // < 2^62
+    const int64_t df = l.hidden * l.ffn;  // <= 2^48
     int64_t last = l.gate_off > l.down_off ? l.gate_off : l.down_off;
     last = l.up_off > last ? l.up_off : last;
-    if (df > ((int64_t)1 << 58))
-        return fail(MP_E_ARG, "hidden * ffn is too large");
     const size_t ebytes = (size_t)(last + df) * (size_t)es;
     MoeArgs a{l, (int)tokens, E, x, ldx, router, router_bias, residual, ldr, y, ldy, ids, gates};
     ExpertPtrs ex{};

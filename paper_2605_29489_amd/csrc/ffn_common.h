@@ -136,8 +136,9 @@ __device__ inline float act_slope_f(float z)
         return 0.5f * (1.0f + erff(z * 0.70710678118655f)) +
                z * 0.398942280401433f * __builtin_amdgcn_exp2f(z * z * -0.72134752044448f);
     else if constexpr (ACT == MP_ACT_GELU_TANH) {
+        // where z z overflows, p (1 - p) is 0: bounded, so that their product is too
         const float p = sigmoid_f(kGeluC * (z + 0.044715f * z * z * z));
-        return p + z * p * (1.0f - p) * kGeluC * (1.0f + 0.134145f * z * z);
+        return p + z * p * (1.0f - p) * kGeluC * (1.0f + 0.134145f * fminf(z * z, 1e30f));
     } else if constexpr (ACT == MP_ACT_SILU) {
         const float p = sigmoid_f(z);
         return p + z * p * (1.0f - p);

@@ -89,3 +89,18 @@ def test_moe_token_limit(mp):
     assert mp.lib.mp_moe_workspace(C.byref(s), 64, C.byref(n)) == mp.MP_OK and n.value > 0
     assert mp.lib.mp_moe_workspace(C.byref(s), 65, C.byref(n)) == mp.MP_E_UNSUPPORTED
     assert mp.lib.mp_moe_workspace(C.byref(s), -1, C.byref(n)) == mp.MP_E_ARG
+
+
+def test_sizes_that_no_launch_holds_are_refused(mp):
+    one, n = C.c_void_p(16), C.c_uint64(0)
+    for over in (dict(m=(1 << 26) + 1), dict(n=(1 << 26) + 1, ldy=1 << 27), dict(k=(1 << 26) + 1, ldx=1 << 27)):
+        s = _linear(mp, **over)
+        assert mp.lib.mp_linear(C.byref(s), one, one, None, None, one, None, None, 0, None) == mp.MP_E_ARG
+        assert mp.lib.mp_linear_workspace(C.byref(s), 1, C.byref(n)) == mp.MP_E_ARG
+    s = mp.mp_norm_shape(1, 0, 4, (1 << 26) + 1, 1 << 27, 1 << 27, 1e-6)
+    assert mp.lib.mp_norm_workspace(C.byref(s), C.byref(n)) == mp.MP_E_ARG
+    for over in (dict(hidden=(1 << 24) + 1), dict(ffn=(1 << 24) + 1)):
+        f = dict(dtype=1, act=4, top_k=2, flags=0, hidden=8, ffn=6, gate_off=0, up_off=48, down_off=96)
+        f.update(over)
+        s = mp.mp_moe_layer(**f)
+        assert mp.lib.mp_moe_workspace(C.byref(s), 4, C.byref(n)) == mp.MP_E_ARG

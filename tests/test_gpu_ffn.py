@@ -701,3 +701,36 @@ def test_refusals(mp):
         mp.mp_moe(lay, x, r, [e[:100] for e in ex], o)
     torch.cuda.synchronize()
     assert (y == 7).all() and (o == 7).all() and (buf == 1).all()
+
+
+def test_row_strides_whose_extent_passes_64_bits_are_refused(mp):
+    """(rows - 1) * ld elements that wrap around to a few bytes: the buffer is too small all the same."""
+    import ctypes as C
+    import torch
+    rows = (1 << 24) + 1
+    one = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    stat, ws = torch.ones(rows, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    x, y, far = C.c_void_p(one.data_ptr()), C.c_void_p(out.data_ptr()), 1 << 40
+    for m, n, lds in ((rows, 1, dict(ldx=far)), (rows, 1, dict(ldy=far)), (1, rows, dict(ldw=far, ldy=rows))):
+        f = dict(dtype=mp.MP_BF16, act=0, m=m, n=n, k=8, ldx=8, ldw=8, ldy=1, ldz=1, ldr=1)
+        f.update(lds)
+        s = mp.mp_linear_shape(**f)
+        assert mp.lib.mp_linear(C.byref(s), x, x, None, None, y, None, x, 128, None) == mp.MP_E_ARG
+    s = mp.mp_norm_shape(mp.MP_BF16, 0, rows, 8, far, far, 1e-6)
+    assert mp.lib.mp_norm(C.byref(s), x, None, None, y, None, None, None) == mp.MP_E_ARG
+    st = C.c_void_p(stat.data_ptr())
+    assert mp.lib.mp_norm_backward(C.byref(s), x, x, None, st, st, y, far, None, None, C.c_void_p(ws.data_ptr()), 1 << 20,
+                                   None) == mp.MP_E_ARG
+    assert "allocation too small" in mp.mp_last_error()
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+
+
+def test_gelu_tanh_slope_of_huge_values(mp):
+    """The derivative is 0 or 1 where z z passes fp32's range, not NaN."""
+    import torch
+    z = torch.tensor([[-3e38, -1e20, -1e13, 0.0, 1e13, 1e20, 3e38]], device="cuda")
+    dy, db = torch.ones_like(z), torch.empty(7, device="cuda")
+    mp.mp_linear_backward(dy, z=z, act=mp.MP_ACT_GELU_TANH, dbias=db)
+    assert db.tolist() == [0.0, 0.0, 0.0, 0.5, 1.0, 1.0, 1.0]
