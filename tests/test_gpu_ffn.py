@@ -734,3 +734,17 @@ def test_gelu_tanh_slope_of_huge_values(mp):
     dy, db = torch.ones_like(z), torch.empty(7, device="cuda")
     mp.mp_linear_backward(dy, z=z, act=mp.MP_ACT_GELU_TANH, dbias=db)
     assert db.tolist() == [0.0, 0.0, 0.0, 0.5, 1.0, 1.0, 1.0]
+
+
+def test_example_merges_runs_and_trains(mp):
+    """The example: the layer of experts with one expert agrees with the linear layers, and training lowers the loss."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "feed_forward.py")
+    spec = importlib.util.spec_from_file_location("feed_forward_example", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    apart, losses = m.main(tokens=96, steps=3, say=lambda s: None)
+    # the linear layers round g, u, h and their output to bf16 (2^-8 each), outputs of up to about 16
+    assert apart <= 4 * 2.0 ** -8 * 16
+    assert losses[0] > losses[1] > losses[2]
