@@ -538,13 +538,19 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tiles of 256 (bf16) where they give half the CUs one, of 128 where they give
 // every CU one, else of 64, with p split into parts of 16 K tiles and more
-// until there are 512 workgroups: the sum of the parts is a launch and 5 us.
+// (fp32, whose K tile is 2048 cycles of matrix cores: 4) until there are 512
+// workgroups: the sum of the parts is a launch and 5 us.
 // us at one layer of m x n x k in bf16, by tile (parts):
 //   2048 4096 4096: 75 (256), 77 (128), 115 (64)
 //   1024 4096 4096: 114 (256), 46 (128), 59 (64)
 //    512 4096 4096: 43 (128), 36 (128, 2), 29 (64), 45 (64, 2)
 //    128 1536 8960: 88 (128), 44 (64), 19 (64, 8)
 //    300 1000  700: 15 (128), 10.5 (64), 11.8 (64, 2)
+// and in fp32 with tiles of 64, parts of 16 and of 4 K tiles at least:
+//    777  515 1029: 28.7, 25.1
+//    300  300 2000: 28.6, 18.0
+//    128 1536 1536: 24.7, 19.5
+//     90  200  300: 14.8, 12.6
 Choice choose(int dtype, int64_t I, int64_t J, int64_t P)
 {
     const int BK = kRowBytes / (dtype == MP_F32 ? 4 : 2);
@@ -557,7 +563,7 @@ Choice choose(int dtype, int64_t I, int64_t J, int64_t P)
     c.tj = ceil_div(J, c.tile);
     int64_t s = 1;
     if (c.tile == 64) {
-        const int64_t want = 512 / (c.ti * c.tj), most = nk / 16;
+        const int64_t want = 512 / (c.ti * c.tj), most = nk / (dtype == MP_F32 ? 4 : 16);
         s = want < most ? want : most;
         s = s > 1 ? s : 1;
     }

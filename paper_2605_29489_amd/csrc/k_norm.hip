@@ -90,7 +90,13 @@ constexpr int norm_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
 
 // y = (x - mean) rstd w + b.  The row is read once and stays in registers;
 // the sum of squares is taken of the differences from the mean, so that a
-// large mean costs no digits.
+// large mean costs no digits.  Bound by memory: 16384 x 3584 bf16 in 52 us (4.5
+// TB/s), 16384 x 1536 in 19 us.  Rows of 512 threads and more, whose w and b are
+// as long as the row, go to the workgroups that the chip holds, which keep w and
+// b and load the next row before the present one is reduced: 3000 x 8961 fp32
+// takes 50 us (4.3 TB/s), with a workgroup per row 56.  Shorter rows are slower
+// that way (3584 columns 60 us for 56, 1536 columns 20.7 for 19.4).
+constexpr bool norm_stays(int tpr) { return tpr >= 512; }
 template <int DT, int TPR, int NV>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs<DT> a)
 {
@@ -98,14 +104,25 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs<DT> a)
     __shared__ float tmp[2][TPR > 64 ? TPR / 64 : 1];
     const int l = threadIdx.x % TPR, cols = a.cols;
     using R = Row<DT, TPR, NV>;
-    // rows of one wave or less need no barrier, so their threads may leave the loop early
-    for (int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * kRows) {
-        R x, w, b;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    R x, w, b, x1;
+    auto fetch = [&]() {
         x.load(a.x + r * a.ldx, l, cols);
         if (a.w)
             w.load(a.w, l, cols);
         if (a.b)
             b.load(a.b, l, cols);
+    };
+    if constexpr (norm_stays(TPR))
+        if (r < a.rows)
+            fetch();
+    // rows of one wave or less need no barrier, so their threads may leave the loop early
+    for (; r < a.rows; r += step) {
+        if constexpr (!norm_stays(TPR))
+            fetch();
+        else if (r + step < a.rows)
+            x1.load(a.x + (r + step) * a.ldx, l, cols);
         float m = 0.0f, f[V];
         if (!a.rms) {
             float s = 0.0f;
@@ -158,6 +175,8 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs<DT> a)
             if (a.rstd)
                 a.rstd[r] = rs;
         }
+        if constexpr (norm_stays(TPR))
+            x = x1;
         if constexpr (TPR > 64)
             __syncthreads();  // tmp is free again
     }
@@ -215,8 +234,9 @@ constexpr int back_threads(int tpr) { return tpr < 512 ? 512 : tpr; }
 
 // dx, and the columns' sums of dy n and dy, in one reading of dy and x.  A
 // workgroup takes every gridDim-th band of rows; a thread keeps the sums of its
-// columns in registers (NV * V <= 16 columns, so that two rows and the sums
-// fit), the workgroup adds its bands' sums through LDS and writes one partial
+// columns in registers (NV * V <= 24 columns, so that two rows and the sums
+// fit; 16384 x 1536 bf16 43 us with the sum of the partial rows, 1001 x 8961 fp32
+// 33 us, a wait for every row and the second launch included), the workgroup adds its bands' sums through LDS and writes one partial
 // row, which k_sum_rows adds.  The next row is loaded before the present one
 // is reduced.
 template <int DT, int TPR, int NV>
@@ -445,9 +465,12 @@ int norm_chunks(int64_t cols, int V) { return (int)((cols + V - 1) / V); }
 template <int DT, int TPR, int NV>
 void norm_go(const NormArgs<DT>& a, hipStream_t st)
 {
+    // rows to as few workgroups as `most` allows, as many to each
     constexpr int kT = norm_threads(TPR);
     const int64_t per = kT / TPR, n = (a.rows + per - 1) / per;
-    hipLaunchKernelGGL((k_norm<DT, TPR, NV>), dim3((unsigned)(n < kMaxGrid ? n : kMaxGrid)), dim3(kT), 0, st, a);
+    const int64_t most = norm_stays(TPR) ? 256 * 1024 / kT : kMaxGrid;
+    const int64_t turns = (n + most - 1) / most;
+    hipLaunchKernelGGL((k_norm<DT, TPR, NV>), dim3((unsigned)((n + turns - 1) / turns)), dim3(kT), 0, st, a);
 }
 
 template <int DT, int TPR>
@@ -487,11 +510,17 @@ hipError_t norm_t(const mp_norm_shape& s, const void* x, const void* w, const vo
     return hipGetLastError();
 }
 
-// Threads per row of the one-pass backward kernel: at most 16 columns each; 0: longer rows.
-int back_tpr(int64_t cols)
+// Threads per row of the one-pass backward kernel, as few as hold it at 16
+// columns each; 24 columns in bf16 where that makes it one wave, whose rows need
+// no barrier (16384 x 1536: 43 us, with two waves 55); 0: longer rows.  24 columns
+// with more waves gain nothing (1001 x 8961 fp32: 38 us with 512 threads, 33 with
+// 1024).
+int back_tpr(int dtype, int64_t cols)
 {
     if (cols <= 8 * 16)
         return 8;
+    if (dtype == MP_BF16 && cols <= 64 * 24)
+        return 64;
     for (int t = 64; t <= 1024; t *= 2)
         if (cols <= t * 16)
             return t;
@@ -499,9 +528,9 @@ int back_tpr(int64_t cols)
 }
 
 // Workgroups of the backward kernel, one partial row each.
-int back_groups(int64_t rows, int64_t cols)
+int back_groups(int dtype, int64_t rows, int64_t cols)
 {
-    const int tpr = back_tpr(cols);
+    const int tpr = back_tpr(dtype, cols);
     if (tpr == 0)
         return (int)(rows < 64 ? rows : 64);
     const int64_t per = back_threads(tpr) / tpr, n = (rows + per - 1) / per, most = tpr == 1024 ? 256 : 512;
@@ -521,12 +550,12 @@ void back_nv(const NormBackArgs<DT>& a, int nv, int groups, hipStream_t st)
 {
     if (nv == 1)
         return back_go<DT, TPR, 1>(a, groups, st);
-    if constexpr (DT == MP_F32) {  // chunks of 4 columns
+    if constexpr (DT == MP_F32 || TPR == 64)
         if (nv == 3)
             return back_go<DT, TPR, 3>(a, groups, st);
+    if constexpr (DT == MP_F32)  // chunks of 4 columns
         if (nv == 4)
             return back_go<DT, TPR, 4>(a, groups, st);
-    }
     return back_go<DT, TPR, 2>(a, groups, st);
 }
 
@@ -535,11 +564,11 @@ hipError_t norm_back_t(const mp_norm_shape& s, const void* dy, const void* x, co
                        const float* rstd, void* dx, int64_t lddx, void* dw, void* db, void* ws, hipStream_t st)
 {
     using T = typename Elem<DT>::T;
-    const int groups = back_groups(s.rows, s.cols), pitch = norm_pitch(s.cols);
+    const int groups = back_groups(s.dtype, s.rows, s.cols), pitch = norm_pitch(s.cols);
     const bool cols = dw || db;
     NormBackArgs<DT> a{(const T*)dy, (const T*)x, (const T*)w, mean,  rstd, (T*)dx,      cols ? (float*)ws : nullptr,
                        s.rows,       s.ldy,       s.ldx,       lddx,  (int)s.cols, pitch};
-    const int tpr = back_tpr(s.cols), n = norm_chunks(s.cols, Fmt<DT>::V);
+    const int tpr = back_tpr(DT, s.cols), n = norm_chunks(s.cols, Fmt<DT>::V);
     if (s.rows > 0) {
         const int nv = tpr ? (n + tpr - 1) / tpr : 0;
         if (tpr == 8)
@@ -601,7 +630,7 @@ hipError_t launch_sum_rows(int dtype, const float* part, int n, int64_t pitch, i
 
 uint64_t norm_ws_bytes(const mp_norm_shape& s)
 {
-    return 8ull * (uint64_t)back_groups(s.rows, s.cols) * (uint64_t)norm_pitch(s.cols);
+    return 8ull * (uint64_t)back_groups(s.dtype, s.rows, s.cols) * (uint64_t)norm_pitch(s.cols);
 }
 
 }  // namespace mp
