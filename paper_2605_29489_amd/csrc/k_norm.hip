@@ -584,12 +584,13 @@ hipError_t norm_back_t(const mp_norm_shape& s, const void* dy, const void* x, co
         else if (tpr == 1024)
             back_nv<DT, 1024>(a, nv, groups, st);
         else {
-            if (dx)
-                hipLaunchKernelGGL(k_norm_back_long<DT>, dim3((unsigned)(s.rows < kMaxGrid ? s.rows : kMaxGrid)),
-                                   dim3(1024), 0, st, a);
+            // the column sums first: dx may be dy itself
             if (cols)
                 hipLaunchKernelGGL(k_norm_cols_long<DT>, dim3((unsigned)((s.cols + 255) / 256), groups), dim3(256), 0,
                                    st, a);
+            if (dx)
+                hipLaunchKernelGGL(k_norm_back_long<DT>, dim3((unsigned)(s.rows < kMaxGrid ? s.rows : kMaxGrid)),
+                                   dim3(1024), 0, st, a);
         }
     }
     if (cols)

@@ -748,3 +748,25 @@ def test_example_merges_runs_and_trains(mp):
     # the linear layers round g, u, h and their output to bf16 (2^-8 each), outputs of up to about 16
     assert apart <= 4 * 2.0 ** -8 * 16
     assert losses[0] > losses[1] > losses[2]
+
+
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,pad,shift", NORM)
+def test_norm_backward_all_gradients_in_place(mp, dtype, rms, rows, cols, pad, shift):
+    """dx over dy, with dweight and dbias of the same call: the bits of a call with a dx of its own."""
+    import torch
+    rng = np.random.default_rng(rows * 257 + cols)
+    x, _ = _rand(rng, rows, cols, dtype, ld=cols + pad, shift=shift)
+    dy, _ = _rand(rng, rows, cols, dtype, ld=cols + pad, shift=shift)
+    w, _ = _vec(rng, cols, dtype, 0.3, 1.0)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    mean = None if rms else mean
+    mp.mp_norm(x, y, weight=w, rms=rms, mean=mean, rstd=rstd)
+    outs = []
+    for dx in (torch.full_like(x, float("nan")), dy):
+        dw, db = (torch.full((cols,), float("nan"), dtype=_dt(dtype), device="cuda") for _ in range(2))
+        mp.mp_norm_backward(dy, x, rstd, mean=mean, weight=w, rms=rms, dx=dx, dweight=dw, dbias=db)
+        outs.append((dx, dw, db))
+    for name, a, b in zip(("dx", "dweight", "dbias"), *outs):
+        assert torch.equal(a, b), name
