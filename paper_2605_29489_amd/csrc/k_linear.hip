@@ -234,9 +234,11 @@ __global__ __launch_bounds__(256) void k_dz(const typename Elem<DT>::T* dy, int6
     }
 }
 
-// Bands of k_dz: enough workgroups to fill the chip, 2 rows a thread at least.
+// Bands of k_dz: enough workgroups to fill the chip, 2 rows a thread at least; 1 where there are no columns.
 int dz_bands(const mp_linear_shape& s)
 {
+    if (s.n == 0)
+        return 1;
     const int V = s.dtype == MP_F32 ? 4 : 8;
     const int64_t across = (s.n + 64 * V - 1) / (64 * V), want = (2048 + across - 1) / across, most = (s.m + 7) / 8;
     const int64_t n = want < most ? want : most;

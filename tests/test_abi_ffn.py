@@ -2,8 +2,11 @@
 device work (runs on the CPU), and their structs' layouts."""
 
 import ctypes as C
+import os
 
 import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -104,3 +107,21 @@ def test_sizes_that_no_launch_holds_are_refused(mp):
         f.update(over)
         s = mp.mp_moe_layer(**f)
         assert mp.lib.mp_moe_workspace(C.byref(s), 4, C.byref(n)) == mp.MP_E_ARG
+
+
+def test_linear_workspace_of_empty_sizes(mp):
+    """Sizes of zero have a workspace size, both ways; asked in a process of its own, which a host exception
+    would end."""
+    import subprocess
+    import sys
+    ask = """
+import itertools
+import paper_2605_29489_amd as mp
+for dtype, act, m, n, k in itertools.product((0, 1), (0, 4), (0, 4, 70), (0, 6), (0, 8)):
+    print(dtype, act, m, n, k, *(mp.mp_linear_workspace(dtype, act, m, n, k, b) for b in (False, True)), flush=True)
+"""
+    r = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, cwd=ROOT)
+    lines = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+    assert r.returncode == 0 and len(lines) == 48, f"status {r.returncode} after {lines[-1:]}: {r.stderr}"
+    for dtype, act, m, n, k, forward, backward in lines:
+        assert forward == 0 and (n > 0 or backward == 0)

@@ -770,3 +770,15 @@ def test_norm_backward_all_gradients_in_place(mp, dtype, rms, rows, cols, pad, s
         outs.append((dx, dw, db))
     for name, a, b in zip(("dx", "dweight", "dbias"), *outs):
         assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_linear_backward_without_outputs(mp, dtype, act):
+    """n = 0: dx is an empty sum, dw and dbias have no elements."""
+    import torch
+    m, n, k = 5, 0, 8
+    new = lambda *s: torch.full(s, float("nan"), dtype=_dt(dtype), device="cuda")  # noqa: E731
+    dx, dw, db = new(m, k), new(n, k), new(n)
+    mp.mp_linear_backward(new(m, n), x=new(m, k), w=new(n, k), z=new(m, n), act=_code(mp, act), dx=dx, dw=dw, dbias=db)
+    assert (dx == 0).all()
