@@ -2,7 +2,10 @@
 // applied to the accumulators.
 #include "ffn_common.h"
 #include "gemm.h"
+#include "gemm_edge.h"
 #include "mm_few.h"
+
+#include <algorithm>
 
 namespace mp {
 namespace {
@@ -18,6 +21,7 @@ struct TileArgs {
     int ti, tj;      // tiles along i and j
     int splits;      // parts of p, each k_tiles long but the last
     int k_tiles;     // K tiles of a part
+    int whole;       // K tiles, of all of p, that are read in whole chunks
     int64_t pitch;   // of a partial result's rows
     Epi e;
 };
@@ -64,8 +68,9 @@ __device__ inline const char* at32(const char* base, uint32_t off) { return base
 // One operand's part of loading a K tile: which chunks a thread takes, global
 // memory to registers, registers to LDS.  Rows past the last repeat it, columns
 // of p-rows past the last are whatever follows them: their outputs are
-// dropped.  Only p past the end has to be zero, for both operands, and only the
-// matrix's end must not be passed: both concern the last K tile alone.
+// dropped.  Only p past the end has to be zero, for both operands, which
+// concerns the last K tile alone, and the matrix's end must not be passed, which
+// concerns the one before it too where p-rows are shorter than a chunk.
 template <int DT, int B, int N, int kThreads, bool ROWS, bool PERM, int SETS>
 struct Loader {
     static constexpr int es = Fmt<DT>::esize, V = Fmt<DT>::V, BK = kRowBytes / es, CPR = B * es / 16;
@@ -99,7 +104,7 @@ struct Loader {
             }
         }
     }
-    // K tile kt, not the matrix's last, into register set `set`
+    // K tile kt, one of the whole ones, into register set `set`
     __device__ inline void load(int set, int64_t kt)
     {
         const char* p = base + kt * step;
@@ -111,8 +116,8 @@ struct Loader {
             r[set][t] = ld16u(at32(p, off[t]));
         }
     }
-    // the last one, of which p has `left` elements
-    __device__ inline void load_last(int set, int64_t kt, int64_t left)
+    // one with edges, from whose first on p has `left` elements
+    __device__ inline void load_edge(int set, int64_t kt, int64_t left)
     {
         const char* p = base + kt * step;
 #pragma unroll
@@ -247,6 +252,7 @@ __global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads), BM == 64 ? 1 : 2) 
 {
     using C = Tile<DT, F, BM, BN>;
     constexpr bool PERM = !C::BR, kPong = BM == 256;
+    constexpr bool kShort = BM == 64 && (C::AR || C::BR);  // p-rows shorter than a chunk come here
     __shared__ __attribute__((aligned(16))) char lds[2 * (C::kBufA + C::kBufB)];
     int bi, bj;
     const int tiles = g.ti * g.tj, split = blockIdx.x / tiles;
@@ -286,11 +292,15 @@ __global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads), BM == 64 ? 1 : 2) 
                 acc[f][h] = mma16<DT>(b[h], a, acc[f][h]);
         }
     };
-    // The matrix's last K tile, which alone has edges, comes behind the loop
-    // over the tiles below `end`.  There, loads past them repeat the last one,
-    // so that no load hangs on a branch: the compiler then counts those in
-    // flight and waits for the oldest set alone.
-    const int end = split == g.splits - 1 ? nk - 1 : nk;
+    // The matrix's last K tile, and where kShort the one before it, have edges
+    // and come behind the loop over the tiles below `end`.  There, loads past
+    // them repeat the last one, so that no load hangs on a branch: the compiler
+    // then counts those in flight and waits for the oldest set alone.
+    int end = split == g.splits - 1 ? nk - 1 : nk;
+    if constexpr (kShort) {
+        const int whole = g.whole - split * g.k_tiles;  // below 0 in a part of edges alone
+        end = whole < 0 ? 0 : whole < end ? whole : end;
+    }
     auto next = [&](int kt) { return kt < end ? kt : end - 1; };
     // K tile kt is multiplied from one buffer while tile kt + 1 goes from its
     // register set to the other and tile kt + 1 + SETS from memory to that set.
@@ -375,15 +385,22 @@ __global__ __launch_bounds__((Tile<DT, F, BM, BN>::kThreads), BM == 64 ? 1 : 2) 
                     turn(kt + u, u & 1, (u + 1) % C::SETS);
         }
     }
-    if (end < nk) {
-        la.load_last(0, end, pn - (int64_t)end * C::BK);
-        lb.load_last(0, end, pn - (int64_t)end * C::BK);
+    auto edge = [&](int kt) {
+        la.load_edge(0, kt, pn - (int64_t)kt * C::BK);
+        lb.load_edge(0, kt, pn - (int64_t)kt * C::BK);
         la.store(0, sa);
         lb.store(0, sb);
         __syncthreads();
         half(0, 0);
         half(0, 1);
-    }
+    };
+    if (end < nk)
+        edge(end);
+    if constexpr (kShort)
+        if (end + 1 < nk) {
+            __syncthreads();  // the buffer has been read
+            edge(end + 1);
+        }
 
     // lane: row i0 + wi + f * 16 + lane % 16, and with PERM 16 adjacent columns
     // (pieces are 4 columns of each of the wave's four 16s), else 4 of each piece
@@ -581,6 +598,18 @@ int64_t span(const Gemm& g, bool a)
     return n == 0 || cols == 0 ? 0 : ((n - 1) * (a ? g.lda : g.ldb) + cols) * (g.dtype == MP_F32 ? 4 : 2);
 }
 
+// K tiles that both operands' loads may take whole.
+int64_t whole_of(const Gemm& g)
+{
+    const int V = g.dtype == MP_F32 ? 4 : 8, BK = kRowBytes / (g.dtype == MP_F32 ? 4 : 2);
+    int64_t n = whole_k_tiles(g.P, V, V, V, BK);  // operands of rows of p: all but the last
+    if (g.form == Form::TN)
+        n = std::min(n, whole_k_tiles(g.P, g.I, g.lda, V, BK));
+    if (g.form != Form::NT)
+        n = std::min(n, whole_k_tiles(g.P, g.J, g.ldb, V, BK));
+    return n;
+}
+
 // The tiled kernel takes 32-bit offsets inside a tile, and operands of 16 bytes at least.
 bool untiled(const Gemm& g)
 {
@@ -615,6 +644,7 @@ hipError_t gemm_go(const Gemm& g, const Choice& c, void* ws, hipStream_t st)
                (int)c.tj,
                c.splits,
                c.k_tiles,
+               (int)whole_of(g),
                c.pitch,
                g.epi};
     constexpr int kEpi = F == Form::NT ? EPI_FULL : EPI_STORE;
@@ -647,7 +677,15 @@ hipError_t gemm_d(const Gemm& g, void* ws, hipStream_t st)
                            g.I, g.J, g.P, (int)tj, g.epi);
         return hipGetLastError();
     }
-    const Choice c = choose(DT, g.I, g.J, g.P);
+    Choice c = choose(DT, g.I, g.J, g.P);
+    if (whole_of(g) + 1 < ceil_div(g.P, kRowBytes / Fmt<DT>::esize)) {
+        // p-rows shorter than a chunk (three columns at most): larger tiles would be
+        // nearly empty, and their kernels know one K tile with edges.  Whether p is
+        // split stays as it was, and so does the workspace.
+        c.tile = 64;
+        c.ti = ceil_div(g.I, 64);
+        c.tj = ceil_div(g.J, 64);
+    }
     switch (g.form) {
         case Form::NT: return gemm_go<DT, Form::NT>(g, c, ws, st);
         case Form::NN: return gemm_go<DT, Form::NN>(g, c, ws, st);

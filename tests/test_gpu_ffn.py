@@ -782,3 +782,15 @@ def test_linear_backward_without_outputs(mp, dtype, act):
     dx, dw, db = new(m, k), new(n, k), new(n)
     mp.mp_linear_backward(new(m, n), x=new(m, k), w=new(n, k), z=new(m, n), act=_code(mp, act), dx=dx, dw=dw, dbias=db)
     assert (dx == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k,act", [
+    (65, 1, 1, "none"), (66, 2, 1, "none"), (65, 3, 2, "silu"), (33, 1, 40, "none"), (34, 300, 1, "gelu"),
+    (70, 300, 3, "none"), (71, 3, 300, "none"), (129, 1, 2, "relu"), (4161, 1, 515, "none"), (4161, 130, 2, "none"),
+    (40000, 65, 2, "none"), (40000, 33, 1, "silu"), (65, 33000, 1, "none"), (33, 33000, 3, "none"),
+])
+def test_linear_backward_narrow_operands(mp, dtype, m, n, k, act):
+    """Contiguous operands of one to three columns, whose rows are shorter than a load, at every tile size that
+    the sizes ask for; the last K tile holds one to seven rows."""
+    test_linear_backward(mp, dtype, m, n, k, act, True, 0, 0)
