@@ -41,6 +41,8 @@
  * Streams.  `stream` is a hipStream_t (NULL = the default stream).  Work is
  *   enqueued on it; calls return once enqueued unless stated otherwise.
  *   Calls that fill a host-side stats struct synchronise the stream first.
+ *   HIP spreads a process's streams over a few hardware queues (4 by
+ *   default): calls on two streams that share one run in order.
  * Errors.  Every call returns MP_OK (0) or a negative MP_E_* code;
  *   mp_last_error() gives a message (thread-local).  On an argument error,
  *   and on MP_E_NOMEM, nothing is enqueued and no output is written.  On

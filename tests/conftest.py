@@ -20,3 +20,19 @@ def _oracle_built():
     if not os.path.exists(LIB) or os.path.getmtime(LIB) < os.path.getmtime(src):
         build()
     yield
+
+
+# GPU tests that need the stream they take to run beside the default one
+BESIDE = {"test_plan_runs_beside_a_merge"}
+
+
+@pytest.fixture(autouse=True)
+def _side_streams(request):
+    if getattr(request.node, "originalname", "") in BESIDE:
+        import torch
+
+        if torch.cuda.is_available():
+            from tests.gpu_util import side_streams_from_the_first_beside
+
+            side_streams_from_the_first_beside()
+    yield

@@ -64,3 +64,33 @@ def assert_merge_equal(got, want, base, dtype, what=""):
     bad = np.abs(gf - wf) > tol
     assert not bad.any(), f"{what}: {int(bad.sum())} fp32 elements outside 1e-6 relative"
     return int((got.view(np.uint32) != want.view(np.uint32)).sum())
+
+
+def side_streams_from_the_first_beside():
+    """Advances torch's pool of side streams so that the next torch.cuda.Stream() is the first of the pool that
+    runs beside the default stream.
+
+    torch hands out its 32 side streams in turn, so that which one a test gets depends on the tests before it,
+    and HIP spreads a process's streams over 4 hardware queues: the work of streams on one queue runs in order,
+    whatever it is.  Every fourth stream of the pool waits for the default stream that way.  Which, is seen with a
+    small torch kernel that has to end while eight passes over a GiB still run on the default stream."""
+    import torch
+    busy, small = torch.zeros(1 << 30, dtype=torch.uint8, device="cuda"), torch.zeros(64, device="cuda")
+    pool = [torch.cuda.Stream()]
+    while len(pool) == 1 or (pool[-1].cuda_stream != pool[0].cuda_stream and len(pool) < 64):
+        pool.append(torch.cuda.Stream())
+    for s in pool[1:]:  # the next stream of the pool is pool[1]
+        early = 0
+        for _ in range(4):  # the first brings what a first launch needs
+            done = torch.cuda.Event()
+            for _ in range(8):
+                busy.add_(1)
+            done.record()
+            with torch.cuda.stream(s):
+                small.add_(1)
+            s.synchronize()
+            early += not done.query()
+            torch.cuda.synchronize()
+        if early >= 3:
+            return
+        torch.cuda.Stream()

@@ -104,3 +104,11 @@ def test_plan_runs_beside_a_merge(mp, blocks):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.equal(beside, alone)
     assert early >= 3, f"the plan ended before the merge in {early} of 5 tries"
+
+
+def test_plan_runs_beside_a_merge_from_any_stream_on(mp):  # noqa: F811
+    """Whichever of torch's streams the tests before left to be the next."""
+    from tests.gpu_util import side_streams_from_the_first_beside
+    for _ in range(8):
+        side_streams_from_the_first_beside()
+        test_plan_runs_beside_a_merge(mp, 250)
