@@ -388,8 +388,10 @@ int mp_lora_merge_ties_tau(const mp_layout* layout, const void* base, const mp_l
  * Running what a merge made: the feed-forward part of a block
  *
  * Products with a checkpoint's weight matrices, its norms, and a layer that
- * routes a few tokens among the experts' own weights, for evaluating a merged
- * checkpoint, training on from it, or serving its experts unmerged.  Matrices
+ * routes a few tokens among the experts' own weights: what a feed-forward
+ * block takes when a merged checkpoint is evaluated or trained on, or its
+ * experts are served unmerged.  Attention, embeddings, the gated product of a
+ * prompt and the loss are the caller's.  Matrices
  * are row-major with unit stride inside a row and `ld` elements from one row
  * to the next (ld >= columns); rows need no alignment beyond an element's, so
  * tensors are used where a checkpoint holds them.  Rows of whole 16-byte

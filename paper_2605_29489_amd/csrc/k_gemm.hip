@@ -558,16 +558,16 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // (fp32, whose K tile is 2048 cycles of matrix cores: 4) until there are 512
 // workgroups: the sum of the parts is a launch and 5 us.
 // us at one layer of m x n x k in bf16, by tile (parts):
-//   2048 4096 4096: 75 (256), 77 (128), 115 (64)
-//   1024 4096 4096: 114 (256), 46 (128), 59 (64)
-//    512 4096 4096: 43 (128), 36 (128, 2), 29 (64), 45 (64, 2)
-//    128 1536 8960: 88 (128), 44 (64), 19 (64, 8)
-//    300 1000  700: 15 (128), 10.5 (64), 11.8 (64, 2)
+//   2048 4096 4096: 77-84 (256), 77 (128), 126 (64)
+//   1024 4096 4096: 73 (256), 46 (128), 64 (64)
+//    512 4096 4096: 40 (128), 32 (64), 43 (64, 2)
+//    128 1536 8960: 79 (128), 51 (64), 18 (64, 8)
+//    300 1000  700: 11.9 (128), 8.4 (64), 12.0 (64, 2)
 // and in fp32 with tiles of 64, parts of 16 and of 4 K tiles at least:
-//    777  515 1029: 28.7, 25.1
-//    300  300 2000: 28.6, 18.0
-//    128 1536 1536: 24.7, 19.5
-//     90  200  300: 14.8, 12.6
+//    777  515 1029: 26, 22
+//    300  300 2000: 28, 18
+//    128 1536 1536: 25, 19
+//     90  200  300: 14.5, 12.1
 Choice choose(int dtype, int64_t I, int64_t J, int64_t P)
 {
     const int BK = kRowBytes / (dtype == MP_F32 ? 4 : 2);

@@ -59,9 +59,14 @@ __global__ __launch_bounds__(64 * W) void k_linear_few(const char* x, int64_t ld
                         });
 }
 
+// Up to so many tokens go to k_linear_few, more to the tiled products.  us through
+// 8960 x 1536, here and there: 33 tokens bf16 11.7 and 12.9, 64 tokens 12.9 and
+// 12.8; fp32, bound by the matrix cores, 34 and 26, 35 and 28.
 constexpr int kFewTokens = 64;
 
-// One to four tokens: a workgroup takes RG rows, its W waves split k.
+// One to four tokens: a workgroup takes RG rows, its W waves split k.  us through
+// 1536 x 8960, with k_linear_few in brackets: fp32 1 token 10.1 (16.2), 4 tokens 11.9
+// (16.4); bf16 1 and 2 tokens 7.9 (7.9), 4 tokens 9.3 (8.2).
 template <int DT, int RG, int TT, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_gemv(const char* x, int64_t ldx, const char* w, int64_t ldw,
                                                         typename Elem<DT>::T* y, int64_t ldy, int M, int64_t N,
@@ -167,10 +172,14 @@ hipError_t linear_few(const mp_linear_shape& s, const void* x, const void* w, vo
 }
 
 // ---------------------------------------------------------------- dz
-// dz = dy * act'(z) in the dtype (bf16: the type the matrix cores multiply; the
-// rounding leaves dx and dw within 2.3e-3 of their norm), and the columns' sums
-// of the unrounded values, bound by memory (8192 x 8960 bf16: 77 us, 5.7 TB/s): a workgroup takes 512 (bf16) or 256 (fp32) columns of every
-// gridDim.y-th band of 4 rows, a chunk per thread, and writes one partial row.
+// dz = dy * act'(z) in the dtype, and the columns' sums of the unrounded values.
+// In bf16 the rounding is that of the type the matrix cores multiply: dx and dw
+// are 2.3e-3 of their norm from the definition (up to 2.8e-3 where few terms are
+// added), 1.7e-3 (2.0e-3) with dz in fp32.  A second bf16 value for what the
+// rounding leaves would double both products, 410 of 8192 x 8960 x 1536's 461 us.
+// Bound by memory (8192 x 8960 bf16: 79 us, 5.6 TB/s): a workgroup takes 512 (bf16)
+// or 256 (fp32) columns of every gridDim.y-th band of 4 rows, a chunk per thread,
+// and writes one partial row.
 template <int DT, int ACT>
 __global__ __launch_bounds__(256) void k_dz(const typename Elem<DT>::T* dy, int64_t lddy,
                                             const typename Elem<DT>::T* z, int64_t ldz, typename Elem<DT>::T* dz,

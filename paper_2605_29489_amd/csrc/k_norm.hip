@@ -90,12 +90,18 @@ constexpr int norm_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
 
 // y = (x - mean) rstd w + b.  The row is read once and stays in registers;
 // the sum of squares is taken of the differences from the mean, so that a
-// large mean costs no digits.  Bound by memory: 16384 x 3584 bf16 in 52 us (4.5
-// TB/s), 16384 x 1536 in 19 us.  Rows of 512 threads and more, whose w and b are
-// as long as the row, go to the workgroups that the chip holds, which keep w and
-// b and load the next row before the present one is reduced: 3000 x 8961 fp32
-// takes 50 us (4.3 TB/s), with a workgroup per row 56.  Shorter rows are slower
-// that way (3584 columns 60 us for 56, 1536 columns 20.7 for 19.4).
+// large mean costs no digits.  Bound by memory, and by w and b, which come
+// through L2 for every row: 16384 x 3584 bf16 in 52 us (4.5 TB/s; RMS norm
+// without b 47), 16384 x 1536 in 20 us.  Rows of 512 threads and more go to the
+// workgroups that the chip holds, which keep w and b and load the next row
+// before the present one is reduced.  us with w and b kept and with a workgroup
+// per row, layer norm with bias:
+//   128 and 256 threads, bf16  16384 x 3584: 60, 56; 8192 x 4104: 41, 35; 8192 x 8192: 49, 52
+//   256 threads, fp32          8192 x 3200: 42, 44; 8192 x 4096: 50, 51
+//   512 threads, bf16          4096 x 8200: 44, 34; 4096 x 12288: 39, 46; 2048 x 16384: 28, 36
+//   512 threads, fp32          4096 x 4104: 27, 31; 3000 x 8192: 39, 42
+//   1024 threads               2048 x 18944 bf16: 41, 49; 3000 x 8961 fp32: 50, 56
+// Up to 256 threads it gains 2 to 6 % in full rows and costs up to 17 % elsewhere.
 constexpr bool norm_stays(int tpr) { return tpr >= 512; }
 template <int DT, int TPR, int NV>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs<DT> a)
@@ -182,7 +188,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs<DT> a)
     }
 }
 
-// Rows longer than a workgroup's registers: read three times, an element per thread.
+// Rows longer than a workgroup's registers (over 32768 bf16 or 16384 fp32
+// columns, wider than the hidden sizes that norms meet): read three times, an
+// element per thread.  RMS norm of 1000 x 40000 bf16 86 us, 1000 x 20000 fp32 55 us.
 template <int DT>
 __global__ __launch_bounds__(1024) void k_norm_long(NormArgs<DT> a)
 {
@@ -235,10 +243,10 @@ constexpr int back_threads(int tpr) { return tpr < 512 ? 512 : tpr; }
 // dx, and the columns' sums of dy n and dy, in one reading of dy and x.  A
 // workgroup takes every gridDim-th band of rows; a thread keeps the sums of its
 // columns in registers (NV * V <= 24 columns, so that two rows and the sums
-// fit; 16384 x 1536 bf16 43 us with the sum of the partial rows, 1001 x 8961 fp32
-// 33 us, a wait for every row and the second launch included), the workgroup adds its bands' sums through LDS and writes one partial
-// row, which k_sum_rows adds.  The next row is loaded before the present one
-// is reduced.
+// fit; 16384 x 1536 bf16 41 us with the sum of the partial rows, 1001 x 8961 fp32
+// 33 us, a wait for every row and the second launch included), the workgroup
+// adds its bands' sums through LDS and writes one partial row, which k_sum_rows
+// adds.  The next row is loaded before the present one is reduced.
 template <int DT, int TPR, int NV>
 __global__ __launch_bounds__(back_threads(TPR)) void k_norm_back(NormBackArgs<DT> a)
 {
@@ -413,7 +421,9 @@ __global__ __launch_bounds__(1024) void k_sum_rows(const float* part, int n, int
         out[(int64_t)blockIdx.x * 32 + g] = (typename Elem<DT>::T)s;
 }
 
-// Rows longer than the one-pass kernel holds: dx, a workgroup per row.
+// Rows longer than the one-pass kernel holds (over 16384 columns): dx, a
+// workgroup per row, which reads x and dy twice; the column sums read them once
+// more.  RMS norm, all gradients: 1000 x 18944 fp32 97 us, 2048 x 18944 bf16 176 us.
 template <int DT>
 __global__ __launch_bounds__(1024) void k_norm_back_long(NormBackArgs<DT> a)
 {
@@ -512,9 +522,11 @@ hipError_t norm_t(const mp_norm_shape& s, const void* x, const void* w, const vo
 
 // Threads per row of the one-pass backward kernel, as few as hold it at 16
 // columns each; 24 columns in bf16 where that makes it one wave, whose rows need
-// no barrier (16384 x 1536: 43 us, with two waves 55); 0: longer rows.  24 columns
-// with more waves gain nothing (1001 x 8961 fp32: 38 us with 512 threads, 33 with
-// 1024).
+// no barrier; 0: longer rows.  16384 bf16 rows of RMS norm in us, one wave and two:
+//   1032 columns 41, 52; 1280: 43, 54; 1536: 41, 54
+//   1544 columns 50, 56; 1792: 53, 57; 2048: 51, 47 (one wave at 32 columns a thread)
+// 24 columns with more waves gain nothing (1001 x 8961 fp32: 38 us with 512
+// threads, 33 with 1024).
 int back_tpr(int dtype, int64_t cols)
 {
     if (cols <= 8 * 16)
