@@ -390,8 +390,8 @@ int mp_lora_merge_ties_tau(const mp_layout* layout, const void* base, const mp_l
  * Products with a checkpoint's weight matrices, its norms, and a layer that
  * routes a few tokens among the experts' own weights: what a feed-forward
  * block takes when a merged checkpoint is evaluated or trained on, or its
- * experts are served unmerged.  Attention, embeddings, the gated product of a
- * prompt and the loss are the caller's.  Matrices
+ * experts are served unmerged.  The gated product of a prompt, embeddings and
+ * the loss are the caller's; attention follows below.  Matrices
  * are row-major with unit stride inside a row and `ld` elements from one row
  * to the next (ld >= columns); rows need no alignment beyond an element's, so
  * tensors are used where a checkpoint holds them.  Rows of whole 16-byte
@@ -536,6 +536,164 @@ int mp_moe(const mp_moe_layer* layer, int64_t tokens, const void* x, int64_t ldx
 
 /* Workspace bytes of mp_moe for this many tokens.  Host only. */
 int mp_moe_workspace(const mp_moe_layer* layer, int64_t tokens, uint64_t* bytes);
+
+/* ---------------------------------------------------------------------------
+ * Running what a merge made: attention of new tokens over a paged cache
+ *
+ * Rotary positions (with their gradient), a cache of keys and values in pages,
+ * and the attention of one new token per sequence over it: with mp_linear and
+ * mp_norm, what a block of a merged checkpoint takes to be served.  What the
+ * section above says of types, rounding, repeatability, streams, graphs,
+ * workspaces and refusals holds here too.  Positions, slots, page tables and
+ * lengths are device data that no call waits for, so that the kernels deal
+ * with what a host check would refuse: it is said of each what comes of a
+ * value out of range.  None of them makes a kernel leave its buffers. */
+
+/* mp_rope_shape.flags: 0 pairs value i of a head with value i + rot_dim / 2
+ * (the Qwen2.5- and Llama-shaped families), MP_ROPE_INTERLEAVED value 2 i with
+ * 2 i + 1. */
+enum { MP_ROPE_INTERLEAVED = 1 };
+
+/* x and y are tokens x heads x head_dim; the values of a head are adjacent,
+ * tokens lie ldx (ldy) and heads hdx (hdy) elements apart, either of them
+ * outside the other: queries and keys are turned where a packed projection
+ * holds them, in one call where their heads follow each other.  The strides of
+ * a single token or head are ignored. */
+typedef struct mp_rope_shape {
+    int32_t dtype; /* mp_dtype of x and y */
+    int32_t flags;
+    int64_t tokens, heads; /* <= 2^31 - 1, <= 65536 */
+    int64_t head_dim;      /* 1 .. 4096 */
+    int64_t rot_dim;       /* even, 0 .. head_dim: the values of a head that are turned, from its first on */
+    int64_t ldx, hdx, ldy, hdy;
+    float amplitude; /* finite: the turned values' factor, 1 without one */
+} mp_rope_shape;
+
+/* y = x with each pair (a, b) of pair number i of token t turned by
+ * w = positions[t] freqs[i]:
+ *   amplitude (a cos w - b sin w), amplitude (a sin w + b cos w).
+ * The values of a head from rot_dim on are copied.
+ *   positions: device int64[tokens], of any sign, |position| < 2^52; freqs:
+ *   device double[rot_dim / 2], radians per position (mp_rope_frequencies).
+ *   y may be x itself (same pointer and strides).
+ * Angles are formed in 64 bits, reduced to a turn, and their sine and cosine
+ * taken in 32, so that far positions lose nothing. */
+int mp_rope(const mp_rope_shape* shape, const void* x, const int64_t* positions, const double* freqs, void* y,
+            void* stream);
+
+/* The gradient of mp_rope: dx is dy with every pair turned back by the same
+ * angle (and multiplied by the amplitude).  dy has the strides ldy and hdy, dx
+ * ldx and hdx; dx may be dy itself (same pointer and strides). */
+int mp_rope_backward(const mp_rope_shape* shape, const void* dy, const int64_t* positions, const double* freqs,
+                     void* dx, void* stream);
+
+/* Frequencies of a model's rotary positions, in 64 bits:
+ *   MP_ROPE_PLAIN  f_i = base^(-2 i / rot_dim)
+ *   MP_ROPE_LINEAR f_i / factor
+ *   MP_ROPE_NTK    those of base * factor^(rot_dim / (rot_dim - 2))
+ *   MP_ROPE_PARTS  with r = original f_i / (2 pi), the turns of a pair in the
+ *                  context of `original` tokens that the model was trained on,
+ *                  and s = (r - low) / (high - low) held to [0, 1]:
+ *                  f_i s + f_i / factor (1 - s)
+ *   MP_ROPE_YARN   f_i (1 - s) + f_i / factor s, s = (i - lo) / (hi - lo) held
+ *                  to [0, 1], where lo and hi are the pair numbers at which r
+ *                  is `high` (rounded down, >= 0) and `low` (rounded up,
+ *                  <= rot_dim - 1); the amplitude is 0.1 ln(factor) + 1. */
+typedef enum {
+    MP_ROPE_PLAIN = 0,
+    MP_ROPE_LINEAR = 1,
+    MP_ROPE_NTK = 2,
+    MP_ROPE_PARTS = 3,
+    MP_ROPE_YARN = 4
+} mp_rope_kind;
+
+typedef struct mp_rope_scaling {
+    int32_t kind;
+    double base;     /* > 1 */
+    double factor;   /* >= 1; ignored by MP_ROPE_PLAIN */
+    double original; /* > 0; MP_ROPE_PARTS and MP_ROPE_YARN only, as low and high */
+    double low, high; /* 0 < low < high */
+} mp_rope_scaling;
+
+/* freqs: HOST double[rot_dim / 2]; amplitude: HOST float (1 but for
+ * MP_ROPE_YARN), or NULL.  Host only. */
+int mp_rope_frequencies(const mp_rope_scaling* scaling, int64_t rot_dim, double* freqs, float* amplitude);
+
+/* A cache of keys and values in `pages` pages of page_size tokens, in device
+ * memory that the caller allocates and hands out.  Token s of page p has its
+ * head h at p * page_stride + s * slot_stride + h * head_stride, in both
+ * arrays; a head's values are adjacent.  Any order of the three strides is
+ * taken (tokens before heads, heads before tokens), as long as no two heads
+ * share memory; k and v may interleave (one array of pages x 2 x ...). */
+typedef struct mp_kv_cache {
+    int32_t dtype; /* mp_dtype of keys, values and queries */
+    int32_t flags; /* 0 */
+    int64_t pages, page_size; /* page_size >= 1, pages * page_size <= 2^40, page_size <= 2^30 */
+    int64_t heads;            /* of keys and values, 1 .. 4096 */
+    int64_t head_dim;         /* 1 .. 256 (MP_E_UNSUPPORTED beyond) */
+    int64_t page_stride, slot_stride, head_stride; /* <= 2^40, 2^24 and 2^38 */
+    void* k;
+    void* v;
+} mp_kv_cache;
+
+/* New tokens of mp_kv_append.  Rows of k and v (ldk, ldv elements apart) hold
+ * a token's heads side by side, so that they, and q, may be parts of one
+ * packed projection. */
+typedef struct mp_kv_rows {
+    int64_t tokens;  /* <= 2^31 - 1 */
+    int64_t q_heads; /* <= 65536; 0 where there is no q */
+    int64_t rot_dim; /* as in mp_rope_shape; 0: nothing is turned, positions and freqs may be NULL */
+    int32_t flags;   /* 0 or MP_ROPE_INTERLEAVED */
+    float amplitude;
+    int64_t ldk, ldv, ldq, ldqo;
+} mp_kv_rows;
+
+/* Stores the keys of new tokens, turned as mp_rope turns them, and their values
+ * in the cache; slots[t] = page * page_size + place in the page.  A token whose
+ * slot is not in [0, pages * page_size) is not stored (padding, say -1).  Slots
+ * are distinct: of two tokens with one slot either may be stored, or some
+ * values of each.
+ *   k, v: tokens x heads x head_dim.  slots, positions: device int64[tokens].
+ *   q: tokens x q_heads x head_dim, or NULL; q_out receives them turned (every
+ *   token's, stored or not) and may be q itself (same pointer and ld). */
+int mp_kv_append(const mp_kv_cache* cache, const mp_kv_rows* rows, const void* k, const void* v,
+                 const int64_t* slots, const int64_t* positions, const double* freqs, const void* q, void* q_out,
+                 void* stream);
+
+/* Attention of rows of queries over the cache, one new token a row. */
+typedef struct mp_kv_attend_shape {
+    int64_t rows;    /* <= 2^20 */
+    int64_t q_heads; /* a multiple of the cache's heads, rows * q_heads <= 2^23 */
+    int64_t width;   /* pages per row of the table, width * page_size <= 2^31 - 1 */
+    int64_t ldq, ldo;
+    int64_t ldt;     /* >= width, or 0: all rows share one table row */
+    int64_t window;  /* 0: every key; else the last `window` keys, the token's own among them */
+    float scale;     /* finite */
+} mp_kv_attend_shape;
+
+/* out[r][h] = sum over j of p_j v_j, p = softmax over j of scale q[r][h] . k_j,
+ * over the keys and values j in [max(0, lens[r] - window), lens[r]) of sequence
+ * r in head h / (q_heads / heads) of the cache; key j lies in page
+ * table[r][j / page_size] at place j % page_size.  The new token's own key is
+ * one of them (append first).  Several new tokens of one sequence, or a short
+ * prompt, are rows with the same pages and lengths one apart.
+ *   q, out: rows x q_heads x head_dim (ldq, ldo; heads side by side); out may be
+ *   q itself (same pointer and ld).  table: device int32[rows][width] (ldt),
+ *   lens: device int32[rows].  lse: device float[rows][q_heads], or NULL:
+ *   log of the sum over j of exp(scale q . k_j).
+ * A length under 0 counts as 0, one over width * page_size as that; keys of a
+ * page not in [0, pages) are left out, and nothing behind a sequence's length
+ * is used, whatever it holds (NaN included).  A row with no keys, or whose
+ * scores are all -inf, gives out = 0 and lse = -inf.
+ * In bf16, p_j enters its product as a sum of two bf16 values (its rounding and
+ * the rounded remainder), so that it keeps 16 bits.
+ * workspace: mp_kv_attend_workspace(cache, shape, &bytes) bytes (its k, v, ld
+ * and scale are not looked at). */
+int mp_kv_attend(const mp_kv_cache* cache, const mp_kv_attend_shape* shape, const void* q, const int32_t* table,
+                 const int32_t* lens, void* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of mp_kv_attend at this shape.  Host only. */
+int mp_kv_attend_workspace(const mp_kv_cache* cache, const mp_kv_attend_shape* shape, uint64_t* bytes);
 
 /* Measurement aid, not part of the method: a plain stream copy of `bytes`
  * bytes (a multiple of 16, at most 2^40) from device memory src to device

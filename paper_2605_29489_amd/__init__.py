@@ -36,6 +36,8 @@ MP_PLAN_PER_BYTE, MP_PLAN_SKIP_ZERO = 1, 2
 MP_ACT_NONE, MP_ACT_RELU, MP_ACT_GELU, MP_ACT_GELU_TANH, MP_ACT_SILU = range(5)
 MP_NORM_RMS = 1
 MP_MOE_RENORM = 1
+MP_ROPE_INTERLEAVED = 1
+MP_ROPE_PLAIN, MP_ROPE_LINEAR, MP_ROPE_NTK, MP_ROPE_PARTS, MP_ROPE_YARN = range(5)
 
 EXPORTS = ("mp_layout_blocks", "mp_index_blocks", "mp_index_ties", "mp_ties_tensor_thresholds", "mp_plan",
            "mp_plan_noalloc", "mp_coverage", "mp_merge_avg", "mp_merge_avg_renorm",
@@ -43,6 +45,8 @@ EXPORTS = ("mp_layout_blocks", "mp_index_blocks", "mp_index_ties", "mp_ties_tens
            "mp_merge_ties_tau", "mp_merge_dare", "mp_lora_materialize", "mp_lora_merge_ties_tau", "mp_stream_copy",
            "mp_linear", "mp_linear_backward", "mp_linear_workspace", "mp_norm", "mp_norm_backward",
            "mp_norm_workspace", "mp_moe", "mp_moe_workspace",
+           "mp_rope", "mp_rope_backward", "mp_rope_frequencies", "mp_kv_append", "mp_kv_attend",
+           "mp_kv_attend_workspace",
            "mp_set_stage_bytes",
            "mp_set_workspace_limit", "mp_workspace_bytes", "mp_ties_tensor_left", "mp_last_error", "mp_release")
 
@@ -88,6 +92,32 @@ class mp_norm_shape(C.Structure):
 class mp_moe_layer(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("top_k", C.c_int32), ("flags", C.c_int32)] + [
         (n, C.c_int64) for n in ("hidden", "ffn", "gate_off", "up_off", "down_off")]
+
+
+class mp_rope_shape(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_int32)] + [
+        (n, C.c_int64) for n in ("tokens", "heads", "head_dim", "rot_dim", "ldx", "hdx", "ldy", "hdy")] + [
+        ("amplitude", C.c_float)]
+
+
+class mp_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in ("base", "factor", "original", "low", "high")]
+
+
+class mp_kv_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_int32)] + [
+        (n, C.c_int64) for n in ("pages", "page_size", "heads", "head_dim", "page_stride", "slot_stride",
+                                 "head_stride")] + [("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class mp_kv_rows(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("q_heads", C.c_int64), ("rot_dim", C.c_int64), ("flags", C.c_int32),
+                ("amplitude", C.c_float)] + [(n, C.c_int64) for n in ("ldk", "ldv", "ldq", "ldqo")]
+
+
+class mp_kv_attend_shape(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("rows", "q_heads", "width", "ldq", "ldo", "ldt", "window")] + [
+        ("scale", C.c_float)]
 
 
 class MPError(RuntimeError):
@@ -138,6 +168,12 @@ def _load():
     L.mp_norm_workspace.argtypes = [nsp, C.POINTER(u64)]
     L.mp_moe.argtypes = [mlp, i64, vp, i64, vp, vp, C.POINTER(vp), i32, i32, vp, i64, vp, i64, vp, vp, vp, u64, vp]
     L.mp_moe_workspace.argtypes = [mlp, i64, C.POINTER(u64)]
+    rsp, kcp, asp = C.POINTER(mp_rope_shape), C.POINTER(mp_kv_cache), C.POINTER(mp_kv_attend_shape)
+    L.mp_rope.argtypes = L.mp_rope_backward.argtypes = [rsp, vp, vp, vp, vp, vp]
+    L.mp_rope_frequencies.argtypes = [C.POINTER(mp_rope_scaling), i64, C.POINTER(C.c_double), C.POINTER(C.c_float)]
+    L.mp_kv_append.argtypes = [kcp, C.POINTER(mp_kv_rows), vp, vp, vp, vp, vp, vp, vp, vp]
+    L.mp_kv_attend.argtypes = [kcp, asp, vp, vp, vp, vp, vp, vp, u64, vp]
+    L.mp_kv_attend_workspace.argtypes = [kcp, asp, C.POINTER(u64)]
     L.mp_last_error.restype = C.c_char_p
     L.mp_stream_copy.argtypes = [vp, vp, u64, vp]
     L.mp_set_stage_bytes.argtypes = [u64]
@@ -156,7 +192,9 @@ def _load():
                  "mp_merge_ties_tau",
                  "mp_merge_dare", "mp_lora_materialize", "mp_lora_merge_ties_tau", "mp_stream_copy",
                  "mp_linear", "mp_linear_backward", "mp_linear_workspace", "mp_norm", "mp_norm_backward",
-                 "mp_norm_workspace", "mp_moe", "mp_moe_workspace"):
+                 "mp_norm_workspace", "mp_moe", "mp_moe_workspace",
+                 "mp_rope", "mp_rope_backward", "mp_rope_frequencies", "mp_kv_append", "mp_kv_attend",
+                 "mp_kv_attend_workspace"):
         getattr(L, name).restype = C.c_int
     return L
 
@@ -582,6 +620,162 @@ def mp_moe(layer: MoeLayer, x, router, experts, y, ids=None, gates=None, router_
 def mp_moe_workspace(layer: MoeLayer, dtype: int, tokens: int) -> int:
     s = layer._struct(dtype)
     return _need(lib.mp_moe_workspace, C.byref(s), tokens)
+
+
+# ------------------------------------------------------------------ attention over a paged cache
+def _heads(t, tokens, heads, dim, dtype, name: str):
+    """Checks tokens x heads x dim values of unit stride inside a head; (token stride, head stride)."""
+    if t.shape != (tokens, heads, dim):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(tokens, heads, dim)}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    st, sh, sd = t.stride()
+    if sd != 1 and dim > 1:
+        raise ValueError(f"{name}: the values of a head must be adjacent")
+    return st, sh
+
+
+def _head_rows(t, tokens, heads, dim, dtype, name: str) -> int:
+    """The same with the heads of a token side by side; its token stride."""
+    st, sh = _heads(t, tokens, heads, dim, dtype, name)
+    if heads > 1 and sh != dim:
+        raise ValueError(f"{name}: the heads of a token must be adjacent")
+    return st if tokens > 1 else max(st, heads * dim)
+
+
+def _turn_args(tokens, positions, freqs):
+    import torch
+    _vector(positions, tokens, torch.int64, "positions")
+    if freqs is not None:
+        _vector(freqs, freqs.numel(), torch.float64, "freqs")
+        if positions is None:
+            raise ValueError("freqs need positions")
+
+
+def mp_rope_frequencies(rot_dim: int, base: float = 10000.0, kind: int = MP_ROPE_PLAIN, factor: float = 1.0,
+                        original: float = 0.0, low: float = 1.0, high: float = 4.0):
+    """(freqs, amplitude): the frequencies of a model's rotary positions, a float64 host tensor of rot_dim / 2 values
+    (radians per position; the calls take it on the device), and the factor of the turned values.
+
+    ``kind``: MP_ROPE_PLAIN, MP_ROPE_LINEAR, MP_ROPE_NTK, MP_ROPE_PARTS or MP_ROPE_YARN; ``factor``: of the context's
+    extension; ``original``: tokens of the context before it, ``low`` and ``high``: turns in it below which a pair is
+    slowed by the whole factor and above which it is kept."""
+    import torch
+    freqs = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.float64)
+    amplitude = C.c_float(0)
+    s = mp_rope_scaling(int(kind), base, factor, original, low, high)
+    _check(lib.mp_rope_frequencies(C.byref(s), int(rot_dim), C.cast(freqs.data_ptr(), C.POINTER(C.c_double)),
+                                   C.byref(amplitude)))
+    return freqs, float(amplitude.value)
+
+
+def _rope(call, x, y, names, positions, freqs, interleaved, amplitude, back, stream):
+    dt = x.dtype
+    T, H, D = x.shape
+    sx, sy = _heads(x, T, H, D, dt, names[0]), _heads(y, T, H, D, dt, names[1])
+    _turn_args(T, positions, freqs)
+    if back:
+        sx, sy = sy, sx
+    s = mp_rope_shape(_dtype_code(x), MP_ROPE_INTERLEAVED if interleaved else 0, T, H, D, 2 * freqs.numel(), *sx, *sy,
+                      amplitude)
+    _check(call(C.byref(s), x.data_ptr(), _ptr(positions), _ptr(freqs), y.data_ptr(), _stream(stream)))
+
+
+def mp_rope(x, y, positions, freqs, interleaved: bool = False, amplitude: float = 1.0, stream=None):
+    """Rotary positions: the first 2 len(freqs) values of each head of ``x`` [tokens, heads, dim] turned by
+    positions * freqs, the others copied, into ``y``, which may be ``x``.
+
+    fp32 or bf16 device tensors of any token and head strides; ``positions``: int64 [tokens]; ``freqs``: float64
+    (``mp_rope_frequencies``).  Pairs are (i, i + len(freqs)), or ``interleaved`` (2 i, 2 i + 1)."""
+    _rope(lib.mp_rope, x, y, ("x", "y"), positions, freqs, interleaved, amplitude, False, stream)
+
+
+def mp_rope_backward(dy, dx, positions, freqs, interleaved: bool = False, amplitude: float = 1.0, stream=None):
+    """Gradient of ``mp_rope``: ``dy`` turned back into ``dx``, which may be ``dy``."""
+    _rope(lib.mp_rope_backward, dy, dx, ("dy", "dx"), positions, freqs, interleaved, amplitude, True, stream)
+
+
+class KvCache:
+    """mp_kv_cache: keys and values [pages, page_size, heads, dim], device tensors of the same type and strides in
+    which the values of a head are adjacent; they may be transposed views (heads before a page's tokens) and parts of
+    one array."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype:
+            raise ValueError(f"k {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}: expected two equal "
+                             "[pages, page_size, heads, dim]")
+        if k.stride() != v.stride() or (k.stride(3) != 1 and k.shape[3] > 1):
+            raise ValueError("k and v need equal strides, and adjacent values in a head")
+        self.k, self.v = k, v
+        self._s = mp_kv_cache(_dtype_code(k), 0, *k.shape, *k.stride()[:3], k.data_ptr(), v.data_ptr())
+        self._ref = C.byref(self._s)
+
+
+def mp_kv_append(cache: KvCache, k, v, slots, positions=None, freqs=None, q=None, q_out=None,
+                 interleaved: bool = False, amplitude: float = 1.0, stream=None):
+    """Stores new tokens' keys ``k``, turned as ``mp_rope`` turns them, and values ``v`` [tokens, heads, dim] in the
+    cache at ``slots`` (int64 [tokens], page * page_size + place; outside the cache: not stored), and the tokens'
+    queries ``q`` [tokens, q_heads, dim], turned, in ``q_out`` (default: in place).  Without ``freqs`` nothing is
+    turned."""
+    import torch
+    dt, (T, H, D) = cache.k.dtype, k.shape
+    ch, cd = cache.k.shape[2:]
+    if (H, D) != (ch, cd):
+        raise ValueError(f"k: {H} heads of {D}, the cache has {ch} of {cd}")
+    ldk, ldv = _head_rows(k, T, H, D, dt, "k"), _head_rows(v, T, H, D, dt, "v")
+    _vector(slots, T, torch.int64, "slots")
+    _turn_args(T, positions, freqs)
+    hq = ldq = ldqo = 0
+    if q is not None:
+        q_out = q if q_out is None else q_out
+        hq = q.shape[1]
+        ldq, ldqo = _head_rows(q, T, hq, D, dt, "q"), _head_rows(q_out, T, hq, D, dt, "q_out")
+    r = mp_kv_rows(T, hq, 0 if freqs is None else 2 * freqs.numel(), MP_ROPE_INTERLEAVED if interleaved else 0,
+                   amplitude, ldk, ldv, ldq, ldqo)
+    _check(lib.mp_kv_append(cache._ref, C.byref(r), k.data_ptr(), v.data_ptr(), slots.data_ptr(),
+                            _ptr(positions) if freqs is not None else None, _ptr(freqs), _ptr(q),
+                            _ptr(q_out) if q is not None else None, _stream(stream)))
+
+
+def mp_kv_attend(cache: KvCache, q, table, lens, out, scale: Optional[float] = None, window: int = 0, lse=None,
+                 workspace=None, stream=None):
+    """Attention of one new token per row over the cache: ``q`` and ``out`` [rows, q_heads, dim] (``out`` may be
+    ``q``), ``table`` int32 [rows, width], the pages of each row's sequence (an expanded row is taken), ``lens`` int32
+    [rows], its length with the new token, whose key has been appended.
+
+    ``scale``: of the scores, default dim^-0.5; ``window``: keys to look back, the token's own among them (0: all);
+    ``lse``: fp32 [rows, q_heads], receives the log of the summed exponentials; ``workspace``: a device tensor of
+    ``mp_kv_attend_workspace`` bytes to reuse between calls (default: a new one)."""
+    import torch
+    dt, D = cache.k.dtype, cache.k.shape[3]
+    R, H = q.shape[:2]
+    ldq, ldo = _head_rows(q, R, H, D, dt, "q"), _head_rows(out, R, H, D, dt, "out")
+    if table.dim() != 2 or table.shape[0] != R or table.dtype is not torch.int32:
+        raise ValueError(f"table: shape {tuple(table.shape)} {table.dtype}, expected int32 of {R} rows")
+    W = table.shape[1]
+    st, sc = table.stride()
+    if W > 1 and sc != 1:
+        raise ValueError("table: the pages of a row must be adjacent")
+    if R > 1 and st != 0 and st < W:
+        raise ValueError(f"table: rows overlap or run backwards (stride {st})")
+    _vector(lens, R, torch.int32, "lens")
+    if lse is not None and lse.shape != (R, H):
+        raise ValueError(f"lse: shape {tuple(lse.shape)}, expected {(R, H)}")
+    _vector(lse, R * H, torch.float32, "lse")
+    s = mp_kv_attend_shape(R, H, W, ldq, ldo, st if R > 1 else max(st, W), int(window),
+                           D ** -0.5 if scale is None else scale)
+    wp, wb, hold = _scratch(_kv_need(cache, s), workspace, q, stream)
+    _check(lib.mp_kv_attend(cache._ref, C.byref(s), q.data_ptr(), table.data_ptr(), lens.data_ptr(), out.data_ptr(),
+                            _ptr(lse), wp, wb, _stream(stream)))
+
+
+def _kv_need(cache: KvCache, s) -> int:
+    return _need(lib.mp_kv_attend_workspace, cache._ref, C.byref(s))
+
+
+def mp_kv_attend_workspace(cache: KvCache, rows: int, q_heads: int, width: int, window: int = 0) -> int:
+    """Workspace bytes of ``mp_kv_attend`` for a table of rows x width pages."""
+    return _kv_need(cache, mp_kv_attend_shape(rows, q_heads, width, 0, 0, 0, window, 1.0))
 
 
 def mp_last_error() -> str:

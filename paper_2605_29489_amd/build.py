@@ -14,7 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmergepipe.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "k_index.hip", "k_plan.hip", "k_merge.hip", "k_merge_ties.hip", "k_tensor_ties.hip", "k_lora.hip", "k_copy.hip", "stage.hip",
-           "api_ffn.hip", "k_linear.hip", "k_gemm.hip", "k_norm.hip", "k_moe.hip"]
+           "api_ffn.hip", "k_linear.hip", "k_gemm.hip", "k_norm.hip", "k_moe.hip",
+           "api_attn.hip", "k_rope.hip", "k_attend.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -299,6 +299,34 @@ struct MoeArgs {
 hipError_t launch_moe(const MoeArgs& a, const ExpertPtrs& ex, void* ws, hipStream_t st);
 uint64_t moe_ws_bytes(const mp_moe_layer& l, int64_t tokens);
 
+// ---------------------------------------------------------------- attention over a paged cache (api_attn.hip)
+// Arguments below are validated.
+
+// Rotary positions (k_rope.hip).  Strides of a single token or head are 0.
+struct RopeArgs {
+    int dtype;
+    bool interleaved;
+    int64_t tokens;
+    int heads, dim, rot;
+    const void* x;
+    int64_t ldx, hdx;
+    void* y;
+    int64_t ldy, hdy;
+    const int64_t* pos;   // null if rot is 0
+    const double* freqs;  // likewise
+    float amplitude;
+    float sign;  // 1, or -1: turned back
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t st);
+hipError_t launch_kv_append(const mp_kv_cache& c, const mp_kv_rows& r, const void* k, const void* v,
+                            const int64_t* slots, const int64_t* pos, const double* freqs, const void* q, void* q_out,
+                            hipStream_t st);
+
+// Attention of new tokens (k_attend.hip).
+hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, const void* q, const int32_t* table,
+                            const int32_t* lens, void* out, float* lse, void* ws, hipStream_t st);
+uint64_t kv_attend_ws_bytes(const mp_kv_cache& c, const mp_kv_attend_shape& s);
+
 // ---------------------------------------------------------------- host helpers (api.hip)
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int hip_fail(hipError_t e, const char* what);
