@@ -653,7 +653,7 @@ def test_graph_capture_and_replays_at_other_lengths(mp):
 def test_refusals_of_device_buffers(mp):
     import torch
     z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d, device="cuda")  # noqa: E731
-    kv = z(2, 8, 16, 2, 64)
+    kv = z(2, 512, 16, 2, 64)
     c = mp.KvCache(kv[0], kv[1])
     pos, f = z(4, d=torch.int64), z(32, d=torch.float64)
     x, big = z(4, 2, 64), z(4, 10, 64)
