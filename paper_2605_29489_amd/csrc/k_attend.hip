@@ -17,6 +17,7 @@
 // equal work of the whole call, whatever the lengths are, so that ragged rows
 // fill the chip evenly; the parts of a row are joined by a second kernel.
 #include <algorithm>
+#include <type_traits>
 
 #include "ffn_common.h"
 #include "mp_internal.h"
@@ -27,8 +28,8 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTarget = 1024;   // chunks that a call is divided into, about
-constexpr int kMinTiles = 4;    // tiles of a chunk at least: one for each wave
+constexpr int kMinTiles = 4;  // tiles of a share at least: one for each wave
+constexpr int kMostShares = 768;
 
 // Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and
 // m = ceil(2^(31+L) / d), n m / 2^(31+L) exceeds n / d by less than
@@ -54,16 +55,21 @@ struct AttendArgs {
     const int32_t* lens;
     void* out;
     float* lse;   // or null
-    int2* split;  // [rows]: first slot and parts of a row in more than one chunk, else parts 0 or 1
-    float2* stat;  // [slots][heads of a unit]: maximum (log2) and sum
-    float* part;   // [slots][heads of a unit][dim]: sums relative to it
-    int64_t pages, page_stride, slot_stride, head_stride, ldq, ldo, ldt;  // elements
+    int2* split;   // [rows][head sets]: first share and parts of what is in more than one share, else parts 1
+    float2* stat;  // [slots][head tiles of a workgroup][unit_heads]: maximum (log2) and sum
+    float* part;   // [slots][head tiles of a workgroup][unit_heads][dim]: sums relative to it
+    int64_t page_stride, head_stride, ldq, ldo, ldt;  // elements
     int64_t window;
+    uint32_t pages;
+    int32_t slot_stride;
     int32_t most;  // keys that a table row has room for
     int32_t rows, page_size, heads, group, dim;
     int32_t tiles_of_group;  // head tiles of the query heads that share a head of the cache
-    int32_t unit_heads;      // query heads of a unit, at most
-    Div by_page;
+    int32_t unit_heads;      // query heads of a head tile, at most
+    int32_t split_waves;     // waves of a workgroup that share a head tile's keys: 1, 2 or 4
+    int32_t head_sets;       // workgroups that the head tiles of a row take
+    int32_t shares;          // 0: a workgroup per row and head set
+    Div by_page, by_tiles;  // by_tiles: tiles_of_group
     float scale;  // times log2(e)
 };
 
@@ -73,7 +79,9 @@ struct Range {
 };
 __device__ inline Range range_of(const AttendArgs& a, int row)
 {
-    const int32_t len = a.lens[row];
+    // the kernel writes no length: read so, a wave's own row comes through the scalar cache
+    const int32_t len = *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+        reinterpret_cast<uintptr_t>(a.lens + row));
     const int32_t n = len < 0 ? 0 : len < a.most ? len : a.most;
     return {n > a.window ? n - (int32_t)a.window : 0, n};
 }
@@ -83,26 +91,37 @@ __device__ inline int32_t tiles_of(Range r)
     return r.n > r.lo ? (r.n + KT - 1) / KT - r.lo / KT : 0;
 }
 
-// Which chunk of which row a workgroup takes.
-struct Unit {
-    int row, chunk, chunks, slot;  // slot: of the row's first chunk
+// Every row counts for a tile at least, so that one without keys is someone's.
+template <int KT>
+__device__ inline uint32_t work_of(const AttendArgs& a, int row)
+{
+    return max(1, tiles_of<KT>(range_of(a, row)));
+}
+
+// The call's tiles are the sequence (row, head set, tile), and a share is a run
+// of it, of `per` tiles from `at` on; it begins in `row`, whose first tile is at
+// row_at.
+struct Share {
+    uint64_t at, end, row_at;
+    uint32_t per;
+    int row;
 };
 
-// Chunk number `at` of all rows' chunks, counted in the order of the rows.  A row
-// of t tiles has max(1, ceil(t / C)) of them, C so that there are about kTarget
-// units of it.  False if there are fewer chunks.
+// False where the shares before hold everything.
 template <int KT>
-__device__ inline bool find_unit(const AttendArgs& a, uint32_t at, uint32_t per_chunk, Unit* out)
+__device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* out)
 {
     __shared__ uint64_t sums[4];
-    __shared__ Unit found;
+    __shared__ uint64_t found_at;
+    __shared__ int found_row;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t sets = (uint32_t)a.head_sets;
     uint64_t total = 0;
-    int32_t first = 0;
+    uint32_t first = 0;
     for (int r = tid; r < a.rows; r += 256) {
-        const int32_t t = tiles_of<KT>(range_of(a, r));
+        const uint32_t t = work_of<KT>(a, r);
         first = r == tid ? t : first;
-        total += (uint32_t)t;
+        total += t;
     }
     if (a.rows > 1) {
 #pragma unroll
@@ -110,27 +129,27 @@ __device__ inline bool find_unit(const AttendArgs& a, uint32_t at, uint32_t per_
             total += __shfl_xor(total, o);
         if (lane == 0)
             sums[wave] = total;
-        if (tid == 0)
-            found.row = -1;
         __syncthreads();
         total = sums[0] + sums[1] + sums[2] + sums[3];
     } else {
-        total = (uint32_t)tiles_of<KT>(range_of(a, 0));
+        total = work_of<KT>(a, 0);
     }
-    const uint64_t even = (total * per_chunk + kTarget - 1) / kTarget;
-    const uint32_t C = even < kMinTiles ? kMinTiles : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
-    if (a.rows == 1) {
-        const uint32_t c = max(1u, ((uint32_t)total + C - 1) / C);
-        *out = {0, (int)at, (int)c, 0};
-        return at < c;
-    }
-    // chunks in the low half, slots of split rows in the high half
+    const uint64_t all = total * sets, even = (all + a.shares - 1) / (uint32_t)a.shares;
+    out->per = even < kMinTiles ? (uint32_t)kMinTiles : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
+    out->at = (uint64_t)number * out->per;
+    out->end = min(all, out->at + out->per);
+    out->row = 0;
+    out->row_at = 0;
+    if (out->at >= all)
+        return false;
+    if (a.rows == 1)
+        return true;
+    // the row r with before(r) <= at / sets < before(r + 1)
+    const uint64_t at = out->at / sets;
     uint64_t before = 0;
     for (int r0 = 0; r0 < a.rows; r0 += 256) {
         const int r = r0 + tid;
-        const uint32_t t = r0 == 0 ? first : r < a.rows ? tiles_of<KT>(range_of(a, r)) : 0;
-        const uint32_t c = r < a.rows ? max(1u, (t + C - 1) / C) : 0;
-        const uint64_t own = c | (uint64_t)(c > 1 ? c : 0) << 32;
+        const uint32_t own = r0 == 0 ? first : r < a.rows ? work_of<KT>(a, r) : 0;
         uint64_t scan = own;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -147,53 +166,59 @@ __device__ inline bool find_unit(const AttendArgs& a, uint32_t at, uint32_t per_
             mine += w < wave ? sums[w] : 0;
             before += sums[w];
         }
-        const uint32_t lo = (uint32_t)mine;
-        if (c != 0 && at >= lo && at - lo < c)
-            found = {r, (int)(at - lo), (int)c, (int)(mine >> 32)};
-        if (at < (uint32_t)before)  // the same in every thread
+        if (at >= mine && at - mine < own) {
+            found_row = r;
+            found_at = mine * sets;
+        }
+        if (at < before)  // the same in every thread
             break;
     }
     __syncthreads();
-    *out = found;
-    return out->row >= 0;
+    out->row = found_row;
+    out->row_at = found_at;
+    return true;
 }
 
-// ---------------------------------------------------------------- chunks of rows
-// PAGES: how a tile's rows are found and read.
-enum { kWhole = 0, kEven = 1, kOdd = 2 };
-// kWhole: pages hold whole groups of 16 keys and heads fill the registers'
-// dims, so that a group's address is one for the wave.  kEven: any page size,
-// heads of whole 16-byte chunks.  kOdd: any heads.
-
-// N (8 or 16) bytes at p, d elements in a row of dim elements; elements past it are 0.
-template <int DT, int PAGES, int N>
-__device__ inline uint4 ld_dims(const char* row, int d, int dim)
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline uint64_t uniform(uint64_t x)
 {
-    constexpr int es = Fmt<DT>::esize, E = N / es;
-    typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-    typedef u32x2_t u32x2_a2 __attribute__((aligned(2)));
-    const auto whole = [](const char* p) -> uint4 {
-        if constexpr (N == 16)
-            return ld16u(p);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
+// ---------------------------------------------------------------- shares of the tiles
+// MODE: how keys and values are found and read.
+enum { kWhole = 0, kRows = 1, kEven = 2, kOdd = 3 };
+// kWhole: pages hold whole groups of 16 keys, so that a group's address is one
+// for the wave, and heads fill the registers' dims.  kRows: the same pages, heads
+// of at least a 16-byte chunk.  kEven: any page size.  kOdd: any heads as well.
+
+// Workgroups that a CU's registers hold.
+constexpr int resident(int dp, int ht) { return dp * ht <= 64 ? 3 : dp * ht <= 128 ? 2 : 1; }
+
+// The chunk at dim d of a row of few dims, one value at a time, zeros behind it.
+template <int DT>
+__device__ inline uint4 ld16_few(const char* row, int d, int dim)
+{
+    return d < dim ? ld16_head<DT>(row + d * Fmt<DT>::esize, dim - d) : make_uint4(0, 0, 0, 0);
+}
+
+// N (8 or 16) bytes of a row of values.  A load instruction takes whole rows of
+// up to 256 bytes, which no other reads, so that they need not stay in the
+// caches; rows of keys are read in pieces of 64 bytes by several, and do.  64
+// rows of up to 8192 keys: 211 us without non-temporal loads, 193 with them for
+// the values, 192 for both; rows of 128 bytes: 86.6, 86.8 and 88.5 us.
+template <int N>
+__device__ inline uint4 ld_values(const char* p)
+{
+    if constexpr (N == 16) {
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(p));
+        return make_uint4(v.x, v.y, v.z, v.w);
+    } else {
+        typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+        typedef u32x2_t u32x2_a2 __attribute__((aligned(2)));
         const u32x2_t v = *reinterpret_cast<const u32x2_a2*>(p);
         return make_uint4(v.x, v.y, 0, 0);
-    };
-    if constexpr (PAGES == kWhole) {
-        return whole(row + d * es);
-    } else if constexpr (PAGES == kEven) {
-        const uint4 c = whole(row + (d < dim ? d : 0) * es);
-        return d < dim ? c : make_uint4(0, 0, 0, 0);
-    } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-            if (d + j < dim) {
-                if constexpr (DT == MP_F32)
-                    w[j] = reinterpret_cast<const uint32_t*>(row)[d + j];
-                else
-                    w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[d + j] << (16 * (j & 1));
-            }
-        return make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -230,14 +255,43 @@ __device__ inline uint32_t finite2(uint32_t w)
     return (w & 0x7f800000u) == 0x7f800000u ? w & 0xffffu : w;
 }
 
+// W dims of an output.
+template <int DT, int W>
+__device__ inline void st_dims(void* p, const float* x)
+{
+    if constexpr (DT == MP_F32) {
+        st16u(p, Fmt<DT>::pack(x));
+    } else if constexpr (W == 8) {
+        st16u(p, Fmt<DT>::pack(x));
+    } else {
+        typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+        typedef u32x2_t u32x2_a2 __attribute__((aligned(2)));
+        *static_cast<u32x2_a2*>(p) = u32x2_t{Fmt<DT>::pack2(x[0], x[1]), Fmt<DT>::pack2(x[2], x[3])};
+    }
+}
+
+// log of a sum l relative to 2^t.
+__device__ inline float lse_of(float t, float l)
+{
+    return l == 0.0f ? -INFINITY : (t + __builtin_amdgcn_logf(l)) * 0.693147180559945f;
+}
+
 // DP: dims that the registers hold (64, 128, 256); HT: tiles of 16 query heads.
 // Lane l = 16 g + m.  First product: m is a key of a group of 16 (operand A) and
 // a query head (B), dims 4 V s + V g + e of step s.  Its result: query head m,
 // keys 4 g + r.  Second product: m is a dim (A) and the query head (B).
-template <int DT, int DP, int HT, int PAGES>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs a)
+//
+// A wave's loads run ahead of it, from one row's tiles into the next row's: keys
+// are asked for when the first product is done with those before, values when
+// the second is, and pages of the cache a tile before that, through the scalar
+// cache.  (Under load a trip to memory takes some 4 us; a row's start would be
+// three, one after the other.)  No branch lies around these loads, so that a
+// wait for keys leaves the values behind them in flight, and the other way
+// round; at a share's end they fetch its last tile again, from the caches.
+template <int DT, int DP, int HT, int MODE>
+__global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
 {
-    constexpr bool kBf16 = DT == MP_BF16;
+    constexpr bool kBf16 = DT == MP_BF16, kUni = MODE == kWhole || MODE == kRows;
     constexpr int es = Fmt<DT>::esize, V = Fmt<DT>::V;
     constexpr int KG = kBf16 ? 2 : 1, KT = 16 * KG;  // groups of 16 keys, keys of a tile
     constexpr int S = DP / (4 * V);                  // steps of the first product
@@ -250,387 +304,570 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs a)
     __shared__ float4 so[4 * 16 * HT * PD / 4];
 
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t per_chunk = (uint32_t)(a.heads * a.tiles_of_group);
-    const uint32_t at = blockIdx.x / per_chunk, ht = blockIdx.x - at * per_chunk;
-    Unit u;
-    if (!find_unit<KT>(a, at, per_chunk, &u))
-        return;
-    // the same in all lanes, which the compiler is told: addresses then are the wave's
-    u.row = __builtin_amdgcn_readfirstlane(u.row);
-    u.chunk = __builtin_amdgcn_readfirstlane(u.chunk);
-    u.chunks = __builtin_amdgcn_readfirstlane(u.chunks);
-    u.slot = __builtin_amdgcn_readfirstlane(u.slot);
-    const int kvh = (int)ht / a.tiles_of_group, gh0 = ((int)ht - kvh * a.tiles_of_group) * 16 * HT;
-    const int nh = min(a.group - gh0, 16 * HT);  // query heads of this unit
-    const Range r = range_of(a, u.row);
-    // the row's tiles, divided evenly
-    const int tiles = tiles_of<KT>(r), tile0 = r.lo / KT;
-    const int begin = tile0 + (int)((int64_t)tiles * u.chunk / u.chunks);
-    const int end = tile0 + (int)((int64_t)tiles * (u.chunk + 1) / u.chunks);
-    if (u.chunk == 0 && ht == 0 && tid == 0 && a.split != nullptr)
-        a.split[u.row] = make_int2(u.slot, u.chunks);
+    const int wave = uniform(tid >> 6);
+    const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group), sets = (uint32_t)a.head_sets;
+    const int step = a.split_waves, wt = 4 / step;  // head tiles of a workgroup
+    // the wave's place among those that share its head tile
+    const int mine = wave / step, place = wave % step;
 
-    // the query heads' operand
-    uint4 q[HT][S];
-#pragma unroll
-    for (int h = 0; h < HT; ++h) {
-        const char* qp = static_cast<const char*>(a.q) +
-                         (u.row * a.ldq + (int64_t)(kvh * a.group + gh0 + (16 * h + m < nh ? 16 * h + m : 0)) * a.dim) * es;
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const uint4 c = ld_dims<DT, PAGES, 16>(qp, 4 * V * s + V * g, a.dim);
-            q[h][s] = 16 * h + m < nh ? c : make_uint4(0, 0, 0, 0);
-        }
+    // The tiles of one row and head set that a share takes.
+    struct Run {
+        int row;
+        uint32_t set, off, n_tiles, work;  // the first one's number, how many, and how many the row has
+        int lo, n;                         // the row's keys
+        int begin, end;                    // this wave's tiles, `step` apart
+    };
+    const auto run_of = [&](int row, uint32_t set, uint32_t off, uint32_t left, Range keys) {
+        Run r;
+        r.row = row;
+        r.set = set;
+        r.off = off;
+        r.work = max(1, tiles_of<KT>(keys));
+        r.n_tiles = min(r.work - off, left);
+        r.lo = keys.lo;
+        r.n = keys.n;
+        const int tile0 = keys.lo / KT + (int)off;
+        r.begin = tile0 + place;
+        // no tiles: a row without keys, and a head tile that is not there
+        r.end = set * wt + mine >= head_tiles || keys.n <= keys.lo ? r.begin : tile0 + (int)r.n_tiles;
+        return r;
+    };
+    // The run behind r, if `left` tiles of the share lie behind it.
+    const auto behind = [&](const Run& r, uint32_t left) {
+        if (r.set + 1 < sets)
+            return run_of(r.row, r.set + 1, 0, left, Range{r.lo, r.n});
+        return run_of(r.row + 1, 0, 0, left, range_of(a, r.row + 1));
+    };
+    // Head tile of a set for this wave: head of the cache, first query head of it, query heads.
+    struct Heads {
+        int kvh, gh0, nh;
+    };
+    const auto heads_of = [&](uint32_t tile) {
+        Heads h;
+        h.kvh = (int)a.by_tiles.of(tile);
+        h.gh0 = ((int)tile - h.kvh * a.tiles_of_group) * 16 * HT;
+        h.nh = min(a.group - h.gh0, 16 * HT);
+        return h;
+    };
+
+    Run cur;
+    uint32_t left, before = 0, per = 0;  // tiles of the share from cur on, and before it; tiles of a share
+    if (a.shares == 0) {
+        const int row = (int)(blockIdx.x / sets);
+        cur = run_of(row, blockIdx.x - (uint32_t)row * sets, 0, 0x7fffffff, range_of(a, row));
+        left = cur.n_tiles;
+    } else {
+        Share share;
+        if (!find_share<KT>(a, blockIdx.x, &share))
+            return;
+        // the same in all lanes, which the compiler is told: addresses then are the wave's
+        per = (uint32_t)uniform((int)share.per);
+        left = (uint32_t)uniform((int)(uint32_t)(share.end - share.at));
+        const uint64_t in = uniform(share.at - share.row_at);
+        const int row = uniform(share.row);
+        const Range keys = range_of(a, row);
+        const uint32_t work = max(1, tiles_of<KT>(keys)), set = (uint32_t)(in / work);
+        cur = run_of(row, set, (uint32_t)(in - (uint64_t)set * work), left, keys);
     }
 
-    const int32_t* table = a.table + u.row * a.ldt;
-    const int64_t head_off = (int64_t)kvh * a.head_stride;
-
-    // Pages of this wave's tiles (begin + wave + 4 i): lane 2 i + j (i with one
-    // group a tile) holds that of group j of tile i, 64 / KG tiles ahead.  -1: no
-    // key of the group counts.
-    const auto pages_from = [&](int tile) -> int32_t {
-        const int t = tile + 4 * (lane / KG), key = t * KT + 16 * (lane % KG);
-        int32_t p = -1;
-        if (t < end && key < r.n) {
-            p = table[a.by_page.of((uint32_t)key)];
-            p = (uint64_t)(int64_t)p < (uint64_t)a.pages ? p : -1;
-        }
-        return p;
+    // The tile that is loaded next.
+    struct Cursor {
+        Run run;
+        uint32_t left;
+        int tile;
+        bool none;  // behind the share's last one, at which it stays
     };
-
-    uint4 kr[KG][S], vr[4 * KG][NC];
-    uint32_t seen = 0;  // kWhole: bit j: group j's page is there; else bit 4 j + r: key 4 g + r of group j
-    const uint32_t k_off = (uint32_t)(m * (int32_t)a.slot_stride + V * g) * es;
-    const uint32_t v_off = (uint32_t)(4 * g * (int32_t)a.slot_stride + W * m) * es;
-    // where a key lies, for pages that end anywhere; -1: nowhere
-    const auto key_at = [&](int key) -> int64_t {
-        if (key >= r.n || key < r.lo)
-            return -1;
-        const uint32_t p = a.by_page.of((uint32_t)key);
-        const int64_t page = table[p];
-        if ((uint64_t)page >= (uint64_t)a.pages)
-            return -1;
-        return page * a.page_stride + (int64_t)(key - (int32_t)(p * (uint32_t)a.page_size)) * a.slot_stride + head_off;
-    };
-    const auto group_at = [&](int key, int32_t page) -> int64_t {
-        const int32_t slot = key - (int32_t)(a.by_page.of((uint32_t)key) * (uint32_t)a.page_size);
-        return ((int64_t)page * a.page_stride + (int64_t)slot * a.slot_stride + head_off) * es;
-    };
-    const auto load_k = [&](int tile, const int32_t* pg) {
-#pragma unroll
-        for (int j = 0; j < KG; ++j) {
-            if constexpr (PAGES == kWhole) {
-                const char* base = a.k + group_at(tile * KT + 16 * j, pg[j] < 0 ? 0 : pg[j]);
-#pragma unroll
-                for (int s = 0; s < S; ++s)
-                    kr[j][s] = ld16u(base + k_off + 4 * V * es * s);
-            } else {
-                const int64_t p = key_at(tile * KT + 16 * j + m);
-                const char* row = a.k + (p < 0 ? 0 : p) * es;
-#pragma unroll
-                for (int s = 0; s < S; ++s)
-                    kr[j][s] = ld_dims<DT, PAGES, 16>(row, 4 * V * s + V * g, a.dim);
+    const auto seek = [&](Cursor& c) {  // from a run's end to the next tile
+        Run r = c.run;
+        uint32_t n = c.left;
+        do {
+            n -= r.n_tiles;
+            if (n == 0) {
+                c.none = true;
+                return;
             }
-        }
+            r = behind(r, n);
+        } while (r.begin >= r.end);
+        c.run = r;
+        c.left = n;
+        c.tile = r.begin;
     };
-    const auto load_v = [&](int tile, const int32_t* pg) {
-        seen = 0;
+    const auto advance = [&](Cursor& c) {
+        if (c.none)
+            return;
+        if (c.tile + step < c.run.end)
+            c.tile += step;
+        else
+            seek(c);
+    };
+
+    uint4 q[HT][S], kr[KG][S], vr[4 * KG][NC];
+    // where a lane's chunks begin in a head, and the dims of a chunk that the one before holds: with heads that do
+    // not fill the registers the last chunks lie over each other
+    const auto chunk_at = [&](int s) {
+        const int d = 4 * V * s + V * g;
+        return MODE == kWhole ? d : min(d, max(a.dim - V, 0));
+    };
+    const auto clear = [&](uint4 c, int s) {
+        if constexpr (MODE != kRows && MODE != kEven)
+            return c;
+        constexpr int bits = 8 * es;
+        const int drop = (4 * V * s + V * g - chunk_at(s)) * bits;
+        const auto keep = [&](int w) { return drop <= 32 * w ? ~0u : drop >= 32 * w + 32 ? 0u : ~0u << (drop - 32 * w); };
+        return make_uint4(c.x & keep(0), c.y & keep(1), c.z & keep(2), c.w & keep(3));
+    };
+    const auto value_at = [&](int c, int mm) {
+        const int d = 16 * W * c + W * mm;
+        return MODE == kWhole || MODE == kOdd ? d : min(d, a.dim - W);
+    };
+    const auto load_q = [&](const Run& r) {
+        const Heads hd = heads_of(r.set * wt + mine);
 #pragma unroll
-        for (int j = 0; j < KG; ++j) {
-            if constexpr (PAGES == kWhole) {
-                seen |= pg[j] < 0 ? 0u : 1u << j;
-                const char* base = a.v + group_at(tile * KT + 16 * j, pg[j] < 0 ? 0 : pg[j]);
+        for (int h = 0; h < HT; ++h) {
+            // heads that are not there take the last one's place: their results are not used
+            const char* qp = static_cast<const char*>(a.q) +
+                             (r.row * a.ldq + (int64_t)(hd.kvh * a.group + hd.gh0 + min(16 * h + m, hd.nh - 1)) * a.dim) * es;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-                        vr[4 * j + i][c] = ld_dims<DT, kWhole, WB>(base + i * a.slot_stride * es + v_off, 16 * W * c, 0);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t p = key_at(tile * KT + 16 * j + 4 * g + i);
-                    seen |= p < 0 ? 0u : 1u << (4 * j + i);
-                    const char* row = a.v + (p < 0 ? 0 : p) * es;
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-                        vr[4 * j + i][c] = ld_dims<DT, PAGES, WB>(row, 16 * W * c + W * m, a.dim);
-                }
-            }
+            for (int s = 0; s < S; ++s)
+                q[h][s] = MODE == kOdd ? ld16_few<DT>(qp, 4 * V * s + V * g, a.dim) : ld16u(qp + chunk_at(s) * es);
         }
     };
 
-    f32x4 o[HT][NC * W];
-    float top[HT], sum[HT];
-    constexpr int kAhead = 64 / KG;  // tiles whose pages a wave holds
-    int32_t held, next = 0;
-    const auto page_of = [&](int i, int32_t* pg) {
+    // kUni: the pages of a tile's groups; else the page of a lane's key (lane % KT).  Not looked at before their use.
+    int32_t page[kUni ? KG : 1];
+    const auto load_pages = [&](const Cursor& c) {
+        const int32_t* table = a.table + c.run.row * a.ldt;
+        if constexpr (kUni) {
 #pragma unroll
-        for (int j = 0; j < KG; ++j)
-            pg[j] = PAGES == kWhole ? __builtin_amdgcn_readlane(held, i * KG + j) : 0;
+            for (int j = 0; j < KG; ++j)
+                page[j] = *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(
+                    table + a.by_page.of((uint32_t)min(c.tile * KT + 16 * j, c.run.n - 1))));
+        } else {
+            page[0] = table[a.by_page.of((uint32_t)min(c.tile * KT + lane % KT, c.run.n - 1))];
+        }
     };
-    // In bf16 an infinite value gives NaN with p's remainder, which may be 0 or
-    // negative.  A wave that ends with NaN goes through its keys once more, now
-    // leaving values that are not finite out of the remainder's product.
-    bool again = false;
-pass:
-#pragma unroll
-    for (int h = 0; h < HT; ++h) {
-        top[h] = -INFINITY;
-        sum[h] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NC * W; ++j)
-            o[h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    held = PAGES == kWhole ? pages_from(begin + wave) : 0;
-    int32_t pg[KG];
-    page_of(0, pg);
-    if (begin + wave < end)
-        load_k(begin + wave, pg);
-    int i = 0;
-    for (int tile = begin + wave; tile < end; tile += 4) {
-        if (PAGES == kWhole && i == 0)
-            next = pages_from(tile + 4 * kAhead);
-        load_v(tile, pg);
-        // scores
-        f32x4 s[HT][KG];
-#pragma unroll
-        for (int h = 0; h < HT; ++h)
+    const uint32_t row_bytes = (uint32_t)a.slot_stride * es;
+    uint32_t seen = 0, seen_next = 0;  // kUni: bit j: group j's page is there; else bit 4 j + r: key 4 g + r of it
+    int64_t where[KG];  // kUni: the groups' offsets; else where[0]: that of the lane's key, -1 if it does not count
+    const auto load_k = [&](const Cursor& c) {
+        const int64_t head = heads_of(c.run.set * wt + mine).kvh * a.head_stride * es;
+        if constexpr (kUni) {
+            seen_next = 0;
 #pragma unroll
             for (int j = 0; j < KG; ++j) {
-                s[h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                const int key = c.tile * KT + 16 * j;
+                const bool there = key < c.run.n && (uint32_t)page[j] < a.pages;
+                const int32_t slot = key - (int32_t)(a.by_page.of((uint32_t)key) * (uint32_t)a.page_size);
+                seen_next |= there ? 1u << j : 0u;
+                where[j] = (there ? page[j] : 0) * (a.page_stride * es) + (int64_t)slot * row_bytes + head;
+                const char* base = a.k + where[j];
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+                    if constexpr (MODE == kWhole)
+                        kr[j][s] = ld16u(base + (uint32_t)(m * row_bytes + V * g * es) + 4 * V * es * s);
+                    else
+                        kr[j][s] = ld16u(base + (uint32_t)(m * row_bytes + chunk_at(s) * es));
+            }
+        } else {
+            const int key = c.tile * KT + lane % KT;
+            const int32_t slot = key - (int32_t)(a.by_page.of((uint32_t)key) * (uint32_t)a.page_size);
+            const bool there = key >= c.run.lo && key < c.run.n && (uint32_t)page[0] < a.pages;
+            where[0] = there ? page[0] * (a.page_stride * es) + (int64_t)slot * row_bytes + head : -1;
+#pragma unroll
+            for (int j = 0; j < KG; ++j) {
+                const char* row = a.k + max((int64_t)__shfl(where[0], 16 * j + m), (int64_t)0);
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+                    kr[j][s] = MODE == kOdd ? ld16_few<DT>(row, 4 * V * s + V * g, a.dim) : ld16u(row + chunk_at(s) * es);
+            }
+        }
+    };
+    const auto load_v = [&]() {
+        if constexpr (kUni) {
+            seen = seen_next;
+#pragma unroll
+            for (int j = 0; j < KG; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        if constexpr (MODE == kWhole)
+                            vr[4 * j + e][c] = ld_values<WB>(a.v + where[j] + e * (int64_t)row_bytes +
+                                                             (uint32_t)(4 * g * row_bytes + WB * m) + 16 * WB * c);
+                        else
+                            vr[4 * j + e][c] = ld_values<WB>(a.v + where[j] + e * (int64_t)row_bytes +
+                                                             (uint32_t)(4 * g * row_bytes + value_at(c, m) * es));
+        } else {
+            seen = 0;
+#pragma unroll
+            for (int j = 0; j < KG; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t p = __shfl(where[0], 16 * j + 4 * g + e);
+                    seen |= p < 0 ? 0u : 1u << (4 * j + e);
+                    const char* row = a.v + max(p, (int64_t)0);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        if constexpr (MODE == kOdd)
+                            vr[4 * j + e][c] = ld16_few<DT>(row, 16 * W * c + W * m, min(a.dim, 16 * W * c + W * m + W));
+                        else
+                            vr[4 * j + e][c] = ld_values<WB>(row + value_at(c, m) * es);
+                }
+        }
+    };
+
+    Cursor ahead;
+    const auto begin_at = [&]() {
+        ahead = Cursor{cur, left, cur.begin, false};
+        if (cur.begin >= cur.end)
+            seek(ahead);
+        if (ahead.none)
+            return;
+        load_pages(ahead);
+        load_q(ahead.run);
+        load_k(ahead);
+        advance(ahead);
+        load_pages(ahead);
+        load_v();
+    };
+    begin_at();
+
+    for (;;) {
+        const bool whole = cur.n_tiles == cur.work;
+        if (cur.off == 0 && tid == 0 && a.split != nullptr)
+            a.split[(int64_t)cur.row * sets + cur.set] =
+                make_int2((int)blockIdx.x, whole ? 1 : (int)((before + cur.work - 1) / per) + 1);
+
+        f32x4 o[HT][NC * W];
+        float top[HT], sum[HT];
+        // In bf16 an infinite value gives NaN with p's remainder, which may be 0 or
+        // negative.  A wave that ends with NaN goes through its keys once more, now
+        // leaving values that are not finite out of the remainder's product.
+        bool again = false;
+pass:
+#pragma unroll
+        for (int h = 0; h < HT; ++h) {
+            top[h] = -INFINITY;
+            sum[h] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NC * W; ++j)
+                o[h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        for (int tile = cur.begin; tile < cur.end; tile += step) {
+            if (MODE != kWhole && tile == cur.begin)
+#pragma unroll
+                for (int h = 0; h < HT; ++h)
+#pragma unroll
+                    for (int s = 0; s < S; ++s)
+                        q[h][s] = clear(q[h][s], s);
+            // scores
+            f32x4 s[HT][KG];
+#pragma unroll
+            for (int j = 0; j < KG; ++j) {
+#pragma unroll
+                for (int h = 0; h < HT; ++h)
+                    s[h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int t = 0; t < S; ++t) {
-                    if constexpr (kBf16) {
-                        s[h][j] = mfma_bf16(kr[j][t], q[h][t], s[h][j]);
-                    } else {
+                    const uint4 k = clear(kr[j][t], t);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            s[h][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(kr[j][t], e)),
-                                                                          __uint_as_float(word(q[h][t], e)), s[h][j], 0,
-                                                                          0, 0);
+                    for (int h = 0; h < HT; ++h) {
+                        if constexpr (kBf16) {
+                            s[h][j] = mfma_bf16(k, q[h][t], s[h][j]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[h][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                    __uint_as_float(word(k, e)), __uint_as_float(word(q[h][t], e)), s[h][j], 0, 0, 0);
+                        }
                     }
                 }
             }
-        // the next tile's keys, in the registers that these left
-        if (++i == kAhead) {
-            i = 0;
-            held = next;
-        }
-        page_of(i, pg);
-        const uint32_t have = seen;
-        if (tile + 4 < end)
-            load_k(tile + 4, pg);
-        // masks: keys outside [lo, n) and of pages that are not there
-        const bool full = PAGES == kWhole && tile * KT >= r.lo && tile * KT + KT <= r.n && have == (1u << KG) - 1;
-        uint32_t in = (1u << (4 * KG)) - 1;  // bit 4 j + r: key 4 g + r of group j
-        if (!full) {
-            if constexpr (PAGES == kWhole) {
-                in = 0;
+            if (ahead.tile == ahead.run.begin)  // of another run
+                load_q(ahead.run);
+            load_k(ahead);
+            advance(ahead);
+            load_pages(ahead);
+            // masks: keys outside [lo, n) and of pages that are not there
+            const bool full = kUni && tile * KT >= cur.lo && tile * KT + KT <= cur.n && seen == (1u << KG) - 1;
+            uint32_t in = (1u << (4 * KG)) - 1;  // bit 4 j + r: key 4 g + r of group j
+            if (!full) {
+                if constexpr (kUni) {
+                    in = 0;
 #pragma unroll
-                for (int j = 0; j < KG; ++j)
+                    for (int j = 0; j < KG; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = tile * KT + 16 * j + 4 * g + e;
-                        in |= (have >> j & 1) != 0 && key >= r.lo && key < r.n ? 1u << (4 * j + e) : 0u;
-                    }
-            } else {
-                in = have;
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = tile * KT + 16 * j + 4 * g + e;
+                            in |= (seen >> j & 1) != 0 && key >= cur.lo && key < cur.n ? 1u << (4 * j + e) : 0u;
+                        }
+                } else {
+                    in = seen;
+                }
+                // what lies there may be NaN, which p = 0 would not hide
+#pragma unroll
+                for (int e = 0; e < 4 * KG; ++e)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        if (!(in >> e & 1))
+                            vr[e][c] = make_uint4(0, 0, 0, 0);
             }
-            // what lies there may be NaN, which p = 0 would not hide
-#pragma unroll
-            for (int e = 0; e < 4 * KG; ++e)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    if (!(in >> e & 1))
-                        vr[e][c] = make_uint4(0, 0, 0, 0);
-        }
-        float p[HT][4 * KG];
-#pragma unroll
-        for (int h = 0; h < HT; ++h) {
-            float best = top[h];
-#pragma unroll
-            for (int e = 0; e < 4 * KG; ++e) {
-                const float x = s[h][e / 4][e % 4] * a.scale;
-                p[h][e] = in >> e & 1 ? x : -INFINITY;
-                best = fmaxf(best, p[h][e]);
-            }
-            best = quad_max(best);
-            if (__any(best > top[h])) {
-                const float keep = best > top[h] ? __builtin_amdgcn_exp2f(top[h] - best) : 1.0f;
-                sum[h] *= keep;
-#pragma unroll
-                for (int j = 0; j < NC * W; ++j)
-                    o[h][j] *= keep;
-                top[h] = best;
-            }
-            const float zero = best == -INFINITY ? 0.0f : best;  // no score above -inf yet
-#pragma unroll
-            for (int e = 0; e < 4 * KG; ++e) {
-                p[h][e] = __builtin_amdgcn_exp2f(p[h][e] - zero);
-                sum[h] += p[h][e];
-            }
-        }
-        // outputs
-        if constexpr (kBf16) {
-            uint4 hi[HT], lo[HT];
+            float p[HT][4 * KG];
 #pragma unroll
             for (int h = 0; h < HT; ++h) {
-                float f[8], back[8];
-                hi[h] = Fmt<DT>::pack(p[h]);
-                Fmt<DT>::unpack(hi[h], back);
+                float best = top[h];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    f[e] = p[h][e] - back[e];
-                lo[h] = Fmt<DT>::pack(f);
+                for (int e = 0; e < 4 * KG; ++e) {
+                    const float x = s[h][e / 4][e % 4] * a.scale;
+                    p[h][e] = in >> e & 1 ? x : -INFINITY;
+                    best = fmaxf(best, p[h][e]);
+                }
+                best = quad_max(best);
+                if (__any(best > top[h])) {
+                    const float keep = best > top[h] ? __builtin_amdgcn_exp2f(top[h] - best) : 1.0f;
+                    sum[h] *= keep;
+#pragma unroll
+                    for (int j = 0; j < NC * W; ++j)
+                        o[h][j] *= keep;
+                    top[h] = best;
+                }
+                const float zero = best == -INFINITY ? 0.0f : best;  // no score above -inf yet
+#pragma unroll
+                for (int e = 0; e < 4 * KG; ++e) {
+                    p[h][e] = __builtin_amdgcn_exp2f(p[h][e] - zero);
+                    sum[h] += p[h][e];
+                }
             }
+            // outputs
+            if constexpr (kBf16) {
+                uint4 hi[HT], lo[HT];
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+                for (int h = 0; h < HT; ++h) {
+                    float f[8], back[8];
+                    hi[h] = Fmt<DT>::pack(p[h]);
+                    Fmt<DT>::unpack(hi[h], back);
 #pragma unroll
-                for (int w = 0; w < W / 2; ++w)
+                    for (int e = 0; e < 8; ++e)
+                        f[e] = p[h][e] - back[e];
+                    lo[h] = Fmt<DT>::pack(f);
+                }
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        // dim 2 w + half of the lane's chunk, keys in pairs
-                        const uint32_t sel = half ? 0x07060302u : 0x05040100u;
-                        uint4 t;
-                        t.x = __builtin_amdgcn_perm(word(vr[1][c], w), word(vr[0][c], w), sel);
-                        t.y = __builtin_amdgcn_perm(word(vr[3][c], w), word(vr[2][c], w), sel);
-                        t.z = __builtin_amdgcn_perm(word(vr[5][c], w), word(vr[4][c], w), sel);
-                        t.w = __builtin_amdgcn_perm(word(vr[7][c], w), word(vr[6][c], w), sel);
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int h = 0; h < HT; ++h)
-                            o[h][c * W + 2 * w + half] = mfma_bf16(t, hi[h], o[h][c * W + 2 * w + half]);
-                        if (again)
-                            t = make_uint4(finite2(t.x), finite2(t.y), finite2(t.z), finite2(t.w));
+                    for (int w = 0; w < W / 2; ++w)
 #pragma unroll
-                        for (int h = 0; h < HT; ++h)
-                            o[h][c * W + 2 * w + half] = mfma_bf16(t, lo[h], o[h][c * W + 2 * w + half]);
-                    }
-        } else {
+                        for (int half = 0; half < 2; ++half) {
+                            // dim 2 w + half of the lane's chunk, keys in pairs
+                            const uint32_t sel = half ? 0x07060302u : 0x05040100u;
+                            uint4 t;
+                            t.x = __builtin_amdgcn_perm(word(vr[1][c], w), word(vr[0][c], w), sel);
+                            t.y = __builtin_amdgcn_perm(word(vr[3][c], w), word(vr[2][c], w), sel);
+                            t.z = __builtin_amdgcn_perm(word(vr[5][c], w), word(vr[4][c], w), sel);
+                            t.w = __builtin_amdgcn_perm(word(vr[7][c], w), word(vr[6][c], w), sel);
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+                            for (int h = 0; h < HT; ++h)
+                                o[h][c * W + 2 * w + half] = mfma_bf16(t, hi[h], o[h][c * W + 2 * w + half]);
+                            if (again)
+                                t = make_uint4(finite2(t.x), finite2(t.y), finite2(t.z), finite2(t.w));
 #pragma unroll
-                for (int j = 0; j < W; ++j)
+                            for (int h = 0; h < HT; ++h)
+                                o[h][c * W + 2 * w + half] = mfma_bf16(t, lo[h], o[h][c * W + 2 * w + half]);
+                        }
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int h = 0; h < HT; ++h)
-                            o[h][c * W + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(vr[e][c], j)),
-                                                                                  p[h][e], o[h][c * W + j], 0, 0, 0);
+                    for (int j = 0; j < W; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int h = 0; h < HT; ++h)
+                                o[h][c * W + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                    __uint_as_float(word(vr[e][c], j)), p[h][e], o[h][c * W + j], 0, 0, 0);
+            }
+            load_v();
         }
-    }
+        const Heads hd = heads_of(min(cur.set * wt + mine, head_tiles - 1));
+        if constexpr (kBf16)
+            if (!again) {
+                bool nan = false;
+#pragma unroll
+                for (int h = 0; h < HT; ++h)
+#pragma unroll
+                    for (int j = 0; j < NC * W; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            nan |= 16 * h + m < hd.nh && o[h][j][e] != o[h][j][e];
+                if (__any(nan)) {
+                    again = true;
+                    begin_at();
+                    goto pass;
+                }
+            }
 
-    if constexpr (kBf16)
-        if (!again) {
-            bool nan = false;
+        using T = typename Elem<DT>::T;
+        // a share holds the end of a row that began before, or the beginning of one that goes on, or both
+        const int64_t slot = (2 * (int64_t)blockIdx.x + (cur.off == 0 ? 1 : 0)) * wt;
+#pragma unroll
+        for (int h = 0; h < HT; ++h)
+            sum[h] = quad_sum(sum[h]);
+        if (step == 1) {
+            // a head tile a wave: from its registers, W dims at a time
+            const int64_t head0 = (int64_t)hd.kvh * a.group + hd.gh0, at = (slot + mine) * a.unit_heads;
+#pragma unroll
+            for (int h = 0; h < HT; ++h) {
+                const int head = 16 * h + m;
+                if (cur.set * wt + mine >= head_tiles || head >= hd.nh)
+                    continue;
+                const float r = sum[h] == 0.0f ? 0.0f : whole ? 1.0f / sum[h] : 1.0f;
+                T* out = static_cast<T*>(a.out) + cur.row * a.ldo + (head0 + head) * a.dim;
+                float* part = a.part + (at + head) * a.dim;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int d = value_at(c, 4 * g + e);
+                        float x[W];
+#pragma unroll
+                        for (int j = 0; j < W; ++j)
+                            x[j] = sum[h] == 0.0f ? 0.0f : o[h][c * W + j][e] * r;
+                        if (MODE != kOdd && whole)
+                            st_dims<DT, W>(out + d, x);
+                        else if (MODE == kWhole)
+                            for (int j = 0; j < W; j += 4)
+                                *reinterpret_cast<float4*>(part + d + j) =
+                                    make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                        else
+                            for (int j = 0; j < W; ++j)
+                                if (MODE != kOdd || d + j < a.dim) {
+                                    if (whole)
+                                        out[d + j] = (T)x[j];
+                                    else
+                                        part[d + j] = x[j];
+                                }
+                    }
+                if (g == 0) {
+                    if (!whole)
+                        a.stat[at + head] = make_float2(top[h], sum[h]);
+                    else if (a.lse != nullptr)
+                        a.lse[cur.row * (int64_t)(a.heads * a.group) + head0 + head] = lse_of(top[h], sum[h]);
+                }
+            }
+        } else {
+            // The waves' parts, in LDS.
 #pragma unroll
             for (int h = 0; h < HT; ++h)
+                if (g == 0) {
+                    sm[wave][16 * h + m] = top[h];
+                    sl[wave][16 * h + m] = sum[h];
+                }
+            __syncthreads();
+            float all_top[HT], all_sum[HT];
 #pragma unroll
-                for (int j = 0; j < NC * W; ++j)
+            for (int h = 0; h < HT; ++h) {
+                float t = -INFINITY, l = 0.0f;
+                for (int w = wave - place; w < wave - place + step; ++w)
+                    t = fmaxf(t, sm[w][16 * h + m]);
+                const float zero = t == -INFINITY ? 0.0f : t;
+                for (int w = wave - place; w < wave - place + step; ++w)
+                    l += sl[w][16 * h + m] * __builtin_amdgcn_exp2f(sm[w][16 * h + m] - zero);
+                all_top[h] = t;
+                all_sum[h] = l;
+                const float f = __builtin_amdgcn_exp2f(top[h] - zero);
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        nan |= 16 * h + m < nh && o[h][j][e] != o[h][j][e];
-            if (__any(nan)) {
-                again = true;
-                goto pass;
+#pragma unroll
+                        for (int j = 0; j < W; j += 4) {
+                            const int at = (wave * 16 * HT + 16 * h + m) * PD + value_at(c, 4 * g + e) + j;
+                            const float4 x = make_float4(o[h][c * W + j][e] * f, o[h][c * W + j + 1][e] * f,
+                                                         o[h][c * W + j + 2][e] * f, o[h][c * W + j + 3][e] * f);
+                            float* to = reinterpret_cast<float*>(so) + at;
+                            if constexpr (MODE == kWhole || MODE == kOdd) {
+                                *reinterpret_cast<float4*>(to) = x;
+                            } else {  // two lanes may hold a dim, with the same value
+                                to[0] = x.x;
+                                to[1] = x.y;
+                                to[2] = x.z;
+                                to[3] = x.w;
+                            }
+                        }
             }
-        }
-
-    // The four waves' parts, in LDS.
+            __syncthreads();  // sm and sl are read
+            if (place == 0 && g == 0)
 #pragma unroll
-    for (int h = 0; h < HT; ++h) {
-        sum[h] = quad_sum(sum[h]);
-        if (g == 0) {
-            sm[wave][16 * h + m] = top[h];
-            sl[wave][16 * h + m] = sum[h];
-        }
-    }
-    __syncthreads();
-    float all_top[HT], all_sum[HT];
-#pragma unroll
-    for (int h = 0; h < HT; ++h) {
-        float t = -INFINITY, l = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            t = fmaxf(t, sm[w][16 * h + m]);
-        const float zero = t == -INFINITY ? 0.0f : t;
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            l += sl[w][16 * h + m] * __builtin_amdgcn_exp2f(sm[w][16 * h + m] - zero);
-        all_top[h] = t;
-        all_sum[h] = l;
-        const float f = __builtin_amdgcn_exp2f(top[h] - zero);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int j = 0; j < W; j += 4)
-                    so[((wave * 16 * HT + 16 * h + m) * PD + 16 * W * c + W * (4 * g + e) + j) / 4] =
-                        make_float4(o[h][c * W + j][e] * f, o[h][c * W + j + 1][e] * f, o[h][c * W + j + 2][e] * f,
-                                    o[h][c * W + j + 3][e] * f);
-    }
-    // the sums of all waves, for the threads that write the outputs
-    __syncthreads();
-    if (wave == 0 && g == 0)
-#pragma unroll
-        for (int h = 0; h < HT; ++h) {
-            sm[0][16 * h + m] = all_top[h];
-            sl[0][16 * h + m] = all_sum[h];
-        }
-    __syncthreads();
-    const float* sof = reinterpret_cast<const float*>(so);
-    const auto total_of = [&](int h, int d) {
-        return sof[h * PD + d] + sof[(16 * HT + h) * PD + d] + sof[(32 * HT + h) * PD + d] +
-               sof[(48 * HT + h) * PD + d];
-    };
-    const int64_t head0 = (int64_t)kvh * a.group + gh0;
-    using T = typename Elem<DT>::T;
-    if (u.chunks == 1) {
-        T* out = static_cast<T*>(a.out) + u.row * a.ldo + head0 * a.dim;
-        for (int d = tid % DP, h = tid / DP; h < nh; h += 256 / DP)
-            if (d < a.dim) {
-                const float l = sl[0][h];
-                out[h * a.dim + d] = (T)(l == 0.0f ? 0.0f : total_of(h, d) / l);
+                for (int h = 0; h < HT; ++h) {
+                    sm[wave][16 * h + m] = all_top[h];
+                    sl[wave][16 * h + m] = all_sum[h];
+                }
+            __syncthreads();
+            // The sums of a head tile's waves, by all threads.
+            const float* sof = reinterpret_cast<const float*>(so);
+            for (int w = 0; w < 4; w += step) {
+                const uint32_t tile = cur.set * wt + w / step;
+                if (tile >= head_tiles)
+                    break;
+                const Heads of = heads_of(tile);
+                const int heads = of.nh;
+                const int64_t head0 = (int64_t)of.kvh * a.group + of.gh0, at = (slot + w / step) * a.unit_heads;
+                T* out = static_cast<T*>(a.out) + cur.row * a.ldo + head0 * a.dim;
+                float* part = a.part + at * a.dim;
+                for (int d = tid % DP, h = tid / DP; h < heads; h += 256 / DP)
+                    if (d < a.dim) {
+                        float x = sof[(w * 16 * HT + h) * PD + d];
+                        for (int v = w + 1; v < w + step; ++v)
+                            x += sof[(v * 16 * HT + h) * PD + d];
+                        if (whole) {
+                            const float l = sl[w][h];
+                            out[h * a.dim + d] = (T)(l == 0.0f ? 0.0f : x / l);
+                        } else {
+                            part[h * a.dim + d] = x;
+                        }
+                    }
+                if (tid < heads) {
+                    const float t = sm[w][tid], l = sl[w][tid];
+                    if (!whole)
+                        a.stat[at + tid] = make_float2(t, l);
+                    else if (a.lse != nullptr)
+                        a.lse[cur.row * (int64_t)(a.heads * a.group) + head0 + tid] = lse_of(t, l);
+                }
             }
-        if (a.lse != nullptr && tid < nh) {
-            const float l = sl[0][tid];
-            a.lse[u.row * (int64_t)(a.heads * a.group) + head0 + tid] =
-                l == 0.0f ? -INFINITY : (sm[0][tid] + __builtin_amdgcn_logf(l)) * 0.693147180559945f;
+            __syncthreads();  // LDS is read
         }
-        return;
+        left -= cur.n_tiles;
+        before += cur.n_tiles;
+        if (left == 0)
+            return;
+        cur = behind(cur, left);
     }
-    const int64_t slot = (int64_t)(u.slot + u.chunk) * per_chunk + ht;
-    float* part = a.part + slot * a.unit_heads * a.dim;
-    for (int d = tid % DP, h = tid / DP; h < nh; h += 256 / DP)
-        if (d < a.dim)
-            part[h * a.dim + d] = total_of(h, d);
-    if (tid < nh)
-        a.stat[slot * a.unit_heads + tid] = make_float2(sm[0][tid], sl[0][tid]);
 }
 
-// A workgroup per row and query head joins the row's parts: sums relative to the
-// largest of their maxima.
+// Joins the parts of a row: their sums relative to the largest of their maxima.
+// A workgroup takes 4 `lanes` dims of one query head, a float4 a thread, the
+// other threads further parts.
 template <int DT>
-__global__ __launch_bounds__(256) void k_join(AttendArgs a)
+__global__ __launch_bounds__(256) void k_join(AttendArgs a, int lanes)
 {
     const uint32_t heads = (uint32_t)(a.heads * a.group);
     const int row = (int)(blockIdx.x / heads), head = (int)(blockIdx.x - (uint32_t)row * heads);
-    const int2 split = a.split[row];
-    if (split.y <= 1)
+    const int kvh = head / a.group, gh = head - kvh * a.group;
+    const int ht = kvh * a.tiles_of_group + gh / a.unit_heads, wt = 4 / a.split_waves;
+    const int2 split = a.split[(int64_t)row * a.head_sets + ht / wt];
+    const int n = split.y;
+    if (n <= 1)
         return;
-    const int tid = threadIdx.x, kvh = head / a.group, gh = head - kvh * a.group;
-    const uint32_t per_chunk = (uint32_t)(a.heads * a.tiles_of_group);
-    const int ht = kvh * a.tiles_of_group + gh / a.unit_heads, h = gh % a.unit_heads;
-    // part c of the row is slot0 + c * per_chunk
-    const int64_t slot0 = (int64_t)split.x * per_chunk + ht;
-    const auto stat = [&](int c) { return a.stat[(slot0 + (int64_t)c * per_chunk) * a.unit_heads + h]; };
+    __shared__ float weight[kMostShares];
     __shared__ float tmp[8];
-    __shared__ float acc[256];
+    __shared__ float4 acc[256];
+    const int tid = threadIdx.x;
+    // part c of the row, in the first place of a share but for part 0
+    const auto place = [&](int c) {
+        return ((2 * (int64_t)(split.x + c) + (c == 0 ? 1 : 0)) * wt + ht % wt) * a.unit_heads + gh % a.unit_heads;
+    };
     float t = -INFINITY;
-    for (int c = tid; c < split.y; c += 256)
-        t = fmaxf(t, stat(c).x);
+    for (int c = tid; c < n; c += 256)
+        t = fmaxf(t, a.stat[place(c)].x);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         t = fmaxf(t, __shfl_xor(t, o));
@@ -640,104 +877,136 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a)
     t = fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
     const float zero = t == -INFINITY ? 0.0f : t;
     float l = 0.0f;
-    for (int c = tid; c < split.y; c += 256) {
-        const float2 s = stat(c);
-        l += s.y * __builtin_amdgcn_exp2f(s.x - zero);
+    for (int c = tid; c < n; c += 256) {
+        const float2 s = a.stat[place(c)];
+        const float w = __builtin_amdgcn_exp2f(s.x - zero);
+        weight[c] = w;
+        l += s.y * w;
     }
     l = wave_xor_sum(l);
     if ((tid & 63) == 0)
         tmp[4 + (tid >> 6)] = l;
     __syncthreads();
     l = tmp[4] + tmp[5] + tmp[6] + tmp[7];
-    // `lanes` threads side by side on the dims, the others on further parts
-    const int lanes = a.dim <= 64 ? 64 : a.dim <= 128 ? 128 : 256, groups = 256 / lanes;
-    const int d = tid % lanes, first = tid / lanes;
-    float sum = 0.0f;
-    if (d < a.dim)
-        for (int c = first; c < split.y; c += groups)
-            sum += a.part[((slot0 + (int64_t)c * per_chunk) * a.unit_heads + h) * a.dim + d] *
-                   __builtin_amdgcn_exp2f(stat(c).x - zero);
-    acc[tid] = sum;
-    __syncthreads();
-    using T = typename Elem<DT>::T;
-    if (first == 0 && d < a.dim) {
-        for (int i = 1; i < groups; ++i)
-            sum += acc[i * lanes + d];
-        static_cast<T*>(a.out)[row * a.ldo + (int64_t)head * a.dim + d] = (T)(l == 0.0f ? 0.0f : sum / l);
+    const int groups = 256 / lanes, mine = tid / lanes, d = (int)(blockIdx.y * lanes + tid % lanes) * 4;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const auto add = [&](float4 v, float w) {
+        sum.x += v.x * w;
+        sum.y += v.y * w;
+        sum.z += v.z * w;
+        sum.w += v.w * w;
+    };
+    const auto part = [&](int c) {
+        const float* q = a.part + place(c) * a.dim + d;
+        if (a.dim % 4 == 0)
+            return *reinterpret_cast<const float4*>(q);
+        const int k = a.dim - d;
+        return make_float4(q[0], k > 1 ? q[1] : 0.0f, k > 2 ? q[2] : 0.0f, k > 3 ? q[3] : 0.0f);
+    };
+    if (d < a.dim) {
+        int c = mine;
+        for (; c + 3 * groups < n; c += 4 * groups) {
+            const float4 v0 = part(c), v1 = part(c + groups), v2 = part(c + 2 * groups), v3 = part(c + 3 * groups);
+            add(v0, weight[c]);
+            add(v1, weight[c + groups]);
+            add(v2, weight[c + 2 * groups]);
+            add(v3, weight[c + 3 * groups]);
+        }
+        for (; c < n; c += groups)
+            add(part(c), weight[c]);
     }
-    if (a.lse != nullptr && tid == 0)
-        a.lse[(int64_t)row * heads + head] = l == 0.0f ? -INFINITY : (t + __builtin_amdgcn_logf(l)) * 0.693147180559945f;
+    acc[tid] = sum;
+    // halves onto halves; the number of groups is a power of two
+    for (int k = groups / 2; k > 0; k /= 2) {
+        __syncthreads();
+        if (mine < k) {
+            const float4 v = acc[tid + k * lanes];
+            add(v, 1.0f);
+            acc[tid] = sum;
+        }
+    }
+    using T = typename Elem<DT>::T;
+    if (mine == 0 && d < a.dim) {
+        T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.dim + d;
+        const float x[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (d + j < a.dim)
+                out[j] = (T)(l == 0.0f ? 0.0f : x[j] / l);
+    }
+    if (a.lse != nullptr && tid == 0 && blockIdx.y == 0)
+        a.lse[(int64_t)row * heads + head] = lse_of(t, l);
 }
 
 // ---------------------------------------------------------------- the host's side
 struct Plan {
-    int ht = 1, tile = 32;
-    int64_t per_chunk = 1, units = 0, slots = 0, unit_heads = 1;
-    bool joins = false;
+    int ht = 1, split_waves = 4;
+    int64_t head_tiles = 1, sets = 1, unit_heads = 1;
+    int64_t shares = 0;  // 0: no row is split
 };
+
+int split_waves_of(int64_t rows, int64_t head_tiles)
+{
+    return rows * head_tiles < 256 ? 4 : head_tiles % 4 == 0 ? 1 : head_tiles % 2 == 0 ? 2 : 4;
+}
 
 Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
 {
     Plan p;
-    const int64_t group = s.q_heads / c.heads;
-    p.tile = c.dtype == MP_F32 ? 16 : 32;
+    const int64_t group = s.q_heads / c.heads, tile = c.dtype == MP_F32 ? 16 : 32;
     p.ht = group > 16 && c.head_dim <= 128 ? 2 : 1;
-    const int64_t tiles_of_group = (group + 16 * p.ht - 1) / (16 * p.ht);
-    p.per_chunk = c.heads * tiles_of_group;
+    p.head_tiles = c.heads * ((group + 16 * p.ht - 1) / (16 * p.ht));
     p.unit_heads = std::min<int64_t>(group, 16 * p.ht);
+    p.split_waves = split_waves_of(s.rows, p.head_tiles);
+    const int64_t wt = 4 / p.split_waves;
+    p.sets = (p.head_tiles + wt - 1) / wt;
     int64_t most = s.width * c.page_size;
-    if (s.window > 0 && s.window < most)
-        most = s.window;
-    const int64_t tiles = (most + p.tile - 1) / p.tile + 1;  // a window may begin inside a tile
-    // chunks of C tiles: rows * per_chunk of them for the rows' first, and as many more as kTarget
-    p.joins = (s.window > 0 ? tiles : tiles - 1) > kMinTiles;
-    p.units = s.rows * p.per_chunk;
-    if (p.joins) {
-        const int64_t longest = (tiles + kMinTiles - 1) / kMinTiles;  // chunks of a row
-        p.units = std::min(p.units + kTarget, p.units * longest);
-        // a row of more than one chunk has less than twice its tiles' share of kTarget
-        p.slots = std::min<int64_t>(2 * kTarget + 2 * p.per_chunk, p.units);
+    const bool slides = s.window > 0 && s.window < most;
+    most = slides ? s.window : most;
+    const int64_t tiles = (most + tile - 1) / tile + (slides ? 1 : 0);  // a window may begin inside a tile
+    if (tiles > kMinTiles) {
+        const int64_t needed = (s.rows * p.sets * tiles + kMinTiles - 1) / kMinTiles;  // < 2^50
+        const int dp = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
+        p.shares = std::min<int64_t>(256 * resident(dp, p.ht), needed);
     }
     return p;
 }
 
 uint64_t up16(uint64_t n) { return (n + 15) / 16 * 16; }
+// query heads of all parts: two of a share, of 4 / split_waves head tiles
+uint64_t slot_heads(const Plan& p) { return (uint64_t)(2 * p.shares * (4 / p.split_waves) * p.unit_heads); }
 
-template <int DT, int DP>
-void launch_dims(const AttendArgs& a, const Plan& p, int pages, hipStream_t st)
+template <int DT, int DP, int HT>
+void launch_tiles(const AttendArgs& a, unsigned grid, int mode, hipStream_t st)
 {
-    const unsigned grid = (unsigned)p.units;
-    if constexpr (DP <= 128)
-        if (p.ht == 2) {
-            if (pages == kWhole)
-                k_attend<DT, DP, 2, kWhole><<<grid, 256, 0, st>>>(a);
-            else if (pages == kEven)
-                k_attend<DT, DP, 2, kEven><<<grid, 256, 0, st>>>(a);
-            else
-                k_attend<DT, DP, 2, kOdd><<<grid, 256, 0, st>>>(a);
-            return;
-        }
-    if (pages == kWhole)
-        k_attend<DT, DP, 1, kWhole><<<grid, 256, 0, st>>>(a);
-    else if (pages == kEven)
-        k_attend<DT, DP, 1, kEven><<<grid, 256, 0, st>>>(a);
-    else
-        k_attend<DT, DP, 1, kOdd><<<grid, 256, 0, st>>>(a);
+    if (mode == kWhole)
+        k_attend<DT, DP, HT, kWhole><<<grid, 256, 0, st>>>(a);
+    else if (mode == kRows)
+        k_attend<DT, DP, HT, kRows><<<grid, 256, 0, st>>>(a);
+    else if (mode == kEven)
+        k_attend<DT, DP, HT, kEven><<<grid, 256, 0, st>>>(a);
+    else if constexpr (DP == 64)
+        k_attend<DT, DP, HT, kOdd><<<grid, 256, 0, st>>>(a);
 }
 
 template <int DT>
 void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
 {
     const int dp = a.dim <= 64 ? 64 : a.dim <= 128 ? 128 : 256;
-    const int pages = a.dim % Fmt<DT>::V != 0 ? kOdd : a.dim == dp && a.page_size % 16 == 0 ? kWhole : kEven;
+    const int mode = a.dim < Fmt<DT>::V ? kOdd : a.page_size % 16 != 0 ? kEven : a.dim == dp ? kWhole : kRows;
+    const unsigned grid = (unsigned)(p.shares ? p.shares : a.rows * p.sets);
     if (dp == 64)
-        launch_dims<DT, 64>(a, p, pages, st);
+        p.ht == 2 ? launch_tiles<DT, 64, 2>(a, grid, mode, st) : launch_tiles<DT, 64, 1>(a, grid, mode, st);
     else if (dp == 128)
-        launch_dims<DT, 128>(a, p, pages, st);
+        p.ht == 2 ? launch_tiles<DT, 128, 2>(a, grid, mode, st) : launch_tiles<DT, 128, 1>(a, grid, mode, st);
     else
-        launch_dims<DT, 256>(a, p, pages, st);
-    if (p.joins)
-        k_join<DT><<<(unsigned)(a.rows * a.heads * a.group), 256, 0, st>>>(a);
+        launch_tiles<DT, 256, 1>(a, grid, mode, st);
+    if (p.shares) {
+        // few heads: their dims in slices of 32, so that more workgroups share the parts
+        const unsigned heads = (unsigned)(a.rows * a.heads * a.group);
+        const int lanes = heads < 512 ? 8 : dp / 4;
+        k_join<DT><<<dim3(heads, (unsigned)((a.dim + 4 * lanes - 1) / (4 * lanes))), 256, 0, st>>>(a, lanes);
+    }
 }
 
 }  // namespace
@@ -745,11 +1014,10 @@ void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
 uint64_t kv_attend_ws_bytes(const mp_kv_cache& c, const mp_kv_attend_shape& s)
 {
     const Plan p = plan_of(c, s);
-    if (s.rows == 0 || !p.joins)
+    if (s.rows == 0 || p.shares == 0)
         return 0;
-    const uint64_t heads = (uint64_t)(p.slots * p.unit_heads);
-    return up16((uint64_t)s.rows * sizeof(int2)) + up16(heads * sizeof(float2)) +
-           heads * (uint64_t)c.head_dim * sizeof(float);
+    return up16((uint64_t)(s.rows * p.sets) * sizeof(int2)) + up16(slot_heads(p) * sizeof(float2)) +
+           slot_heads(p) * (uint64_t)c.head_dim * sizeof(float);
 }
 
 hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, const void* q, const int32_t* table,
@@ -764,17 +1032,17 @@ hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, c
     a.lens = lens;
     a.out = out;
     a.lse = lse;
-    if (p.joins) {
+    if (p.shares) {
         char* w = static_cast<char*>(ws);
         a.split = reinterpret_cast<int2*>(w);
-        w += up16((uint64_t)s.rows * sizeof(int2));
+        w += up16((uint64_t)(s.rows * p.sets) * sizeof(int2));
         a.stat = reinterpret_cast<float2*>(w);
-        w += up16((uint64_t)(p.slots * p.unit_heads) * sizeof(float2));
+        w += up16(slot_heads(p) * sizeof(float2));
         a.part = reinterpret_cast<float*>(w);
     }
-    a.pages = c.pages;
+    a.pages = (uint32_t)std::min<int64_t>(c.pages, INT32_MAX);  // of those that a table can name
     a.page_stride = c.pages > 1 ? c.page_stride : 0;
-    a.slot_stride = c.page_size > 1 ? c.slot_stride : 0;
+    a.slot_stride = c.page_size > 1 ? (int32_t)c.slot_stride : 0;
     a.head_stride = c.heads > 1 ? c.head_stride : 0;
     a.ldq = s.ldq;
     a.ldo = s.ldo;
@@ -786,9 +1054,13 @@ hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, c
     a.heads = (int32_t)c.heads;
     a.group = (int32_t)(s.q_heads / c.heads);
     a.dim = (int32_t)c.head_dim;
-    a.tiles_of_group = (int32_t)(p.per_chunk / c.heads);
+    a.tiles_of_group = (int32_t)(p.head_tiles / c.heads);
+    a.split_waves = p.split_waves;
+    a.head_sets = (int32_t)p.sets;
+    a.shares = (int32_t)p.shares;
     a.unit_heads = (int32_t)p.unit_heads;
     a.by_page = Div((uint32_t)c.page_size);
+    a.by_tiles = Div((uint32_t)a.tiles_of_group);
     a.scale = (float)((double)s.scale * 1.4426950408889634);
     if (c.dtype == MP_F32)
         launch_type<MP_F32>(a, p, st);
