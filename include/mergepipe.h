@@ -664,7 +664,7 @@ int mp_kv_append(const mp_kv_cache* cache, const mp_kv_rows* rows, const void* k
 typedef struct mp_kv_attend_shape {
     int64_t rows;    /* <= 2^20 */
     int64_t q_heads; /* a multiple of the cache's heads, rows * q_heads <= 2^23 */
-    int64_t width;   /* pages per row of the table, width * page_size <= 2^30 */
+    int64_t width;   /* pages per row of the table, width * page_size <= 2^29 */
     int64_t ldq, ldo;
     int64_t ldt;     /* >= width, or 0: all rows share one table row */
     int64_t window;  /* 0: every key; else the last `window` keys, the token's own among them */

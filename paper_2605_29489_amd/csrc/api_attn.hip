@@ -264,8 +264,8 @@ int check_attend(const mp_kv_cache* c, const mp_kv_attend_shape* s, int* es)
                     (long long)c->heads);
     if (s->rows * s->q_heads > (int64_t)1 << 23)
         return fail(MP_E_ARG, "rows * q_heads exceeds 2^23");
-    if (s->width * c->page_size > (int64_t)1 << 30)  // <= 2^61
-        return fail(MP_E_ARG, "width * page_size exceeds 2^30");
+    if (s->width * c->page_size > (int64_t)1 << 29)  // <= 2^61
+        return fail(MP_E_ARG, "width * page_size exceeds 2^29");
     return MP_OK;
 }
 

@@ -28,8 +28,9 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kMinTiles = 4;  // tiles of a share at least: one for each wave
-constexpr int kMostShares = 768;
+constexpr int kMinTiles = 4;  // tiles of a share at least
+constexpr int kShares = 256;  // one for each CU
+constexpr int kInStep = 2;    // tiles that the waves of a workgroup are apart at most
 
 // Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and
 // m = ceil(2^(31+L) / d), n m / 2^(31+L) exceeds n / d by less than
@@ -55,9 +56,9 @@ struct AttendArgs {
     const int32_t* lens;
     void* out;
     float* lse;   // or null
-    int2* split;   // [rows][head sets]: first share and parts of what is in more than one share, else parts 1
-    float2* stat;  // [slots][head tiles of a workgroup][unit_heads]: maximum (log2) and sum
-    float* part;   // [slots][head tiles of a workgroup][unit_heads][dim]: sums relative to it
+    int2* split;   // [rows][head tiles]: first share; number of parts, and above them the head tiles of a set
+    float2* stat;  // [slots][set_tiles][unit_heads]: maximum (log2) and sum
+    float* part;   // [slots][set_tiles][unit_heads][dim]: sums relative to it
     int64_t page_stride, head_stride, ldq, ldo, ldt;  // elements
     int64_t window;
     uint32_t pages;
@@ -66,10 +67,10 @@ struct AttendArgs {
     int32_t rows, page_size, heads, group, dim;
     int32_t tiles_of_group;  // head tiles of the query heads that share a head of the cache
     int32_t unit_heads;      // query heads of a head tile, at most
-    int32_t split_waves;     // waves of a workgroup that share a head tile's keys: 1, 2 or 4
-    int32_t head_sets;       // workgroups that the head tiles of a row take
+    int32_t set_tiles;       // head tiles of a workgroup, a head set: a power of two that divides a row's
+    int32_t one_if_few;      // or one, where the call's tiles are few
     int32_t shares;          // 0: a workgroup per row and head set
-    Div by_page, by_tiles;  // by_tiles: tiles_of_group
+    Div by_page, by_tiles, by_heads;  // page_size, tiles_of_group, unit_heads
     float scale;  // times log2(e)
 };
 
@@ -103,38 +104,69 @@ __device__ inline uint32_t work_of(const AttendArgs& a, int row)
 // row_at.
 struct Share {
     uint64_t at, end, row_at;
-    uint32_t per;
+    uint32_t per, set_tiles;
     int row;
 };
 
-// False where the shares before hold everything.
-template <int KT>
+// Inclusive sum over the lanes before, and its own.
+__device__ inline uint32_t wave_scan(uint32_t v)
+{
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);  // row_bcast:15, 31
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+    return v;
+}
+
+__device__ inline uint64_t quotient(uint64_t n, uint32_t d)
+{
+    return n >> 32 ? n / d : (uint32_t)n / d;  // the same, but 32 bits take a tenth of the instructions
+}
+
+// False where the shares before hold everything.  64 rows' tiles fit 32 bits.
+template <int KT, int NW>
 __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* out)
 {
-    __shared__ uint64_t sums[4];
+    __shared__ uint32_t sums[2][NW];
     __shared__ uint64_t found_at;
     __shared__ int found_row;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t sets = (uint32_t)a.head_sets;
-    uint64_t total = 0;
-    uint32_t first = 0;
-    for (int r = tid; r < a.rows; r += 256) {
-        const uint32_t t = work_of<KT>(a, r);
-        first = r == tid ? t : first;
-        total += t;
-    }
-    if (a.rows > 1) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1)
-            total += __shfl_xor(total, o);
-        if (lane == 0)
-            sums[wave] = total;
+    int turn = 0;
+    // tiles of the thread's row among NW * 64, those of the rows before it from r0 on, and all of them
+    uint32_t own = 0;
+    uint64_t mine = 0, total = 0;
+    const auto scan_from = [&](int r0) {
+        own = r0 + tid < a.rows ? work_of<KT>(a, r0 + tid) : 0;
+        const uint32_t scan = wave_scan(own);
+        if (lane == 63)
+            sums[turn][wave] = scan;
         __syncthreads();
-        total = sums[0] + sums[1] + sums[2] + sums[3];
-    } else {
+        mine = scan - own;
+        uint64_t n = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const uint32_t x = sums[turn][w];
+            mine += w < wave ? x : 0;
+            n += x;
+        }
+        turn ^= 1;  // the next scan's barrier is behind every read of this one's sums
+        return n;
+    };
+    if (a.rows == 1)
         total = work_of<KT>(a, 0);
-    }
-    const uint64_t all = total * sets, even = (all + a.shares - 1) / (uint32_t)a.shares;
+    else
+        for (int r0 = 0; r0 < a.rows; r0 += 64 * NW)
+            total += scan_from(r0);
+    // Whole sets read the heads of a token together, whose places in memory follow
+    // each other; one head tile is divided among a workgroup's waves more finely,
+    // which counts below two tiles a wave: one row of 4096 keys 14.6 and 17.7 us,
+    // of 32768 23.6 and 23.6, of 131072 59 and 55.
+    const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group);
+    out->set_tiles = a.one_if_few && total * head_tiles < 2 * kShares * NW ? 1 : (uint32_t)a.set_tiles;
+    const uint32_t sets = head_tiles / out->set_tiles;
+    const uint64_t all = total * sets, even = quotient(all + a.shares - 1, (uint32_t)a.shares);
     out->per = even < kMinTiles ? (uint32_t)kMinTiles : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
     out->at = (uint64_t)number * out->per;
     out->end = min(all, out->at + out->per);
@@ -145,33 +177,18 @@ __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* o
     if (a.rows == 1)
         return true;
     // the row r with before(r) <= at / sets < before(r + 1)
-    const uint64_t at = out->at / sets;
+    const uint64_t at = quotient(out->at, sets);
     uint64_t before = 0;
-    for (int r0 = 0; r0 < a.rows; r0 += 256) {
-        const int r = r0 + tid;
-        const uint32_t own = r0 == 0 ? first : r < a.rows ? work_of<KT>(a, r) : 0;
-        uint64_t scan = own;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint64_t up = __shfl_up(scan, o);
-            scan += lane >= o ? up : 0;
-        }
-        __syncthreads();  // sums is read
-        if (lane == 63)
-            sums[wave] = scan;
-        __syncthreads();
-        uint64_t mine = before + scan - own;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            mine += w < wave ? sums[w] : 0;
-            before += sums[w];
-        }
-        if (at >= mine && at - mine < own) {
-            found_row = r;
-            found_at = mine * sets;
-        }
-        if (at < before)  // the same in every thread
+    for (int r0 = 0;; r0 += 64 * NW) {
+        const uint64_t n = a.rows > 64 * NW ? scan_from(r0) : total;
+        if (at < before + n) {  // the same in every thread
+            if (at >= before + mine && at - before - mine < own) {
+                found_row = r0 + tid;
+                found_at = (before + mine) * sets;
+            }
             break;
+        }
+        before += n;
     }
     __syncthreads();
     out->row = found_row;
@@ -193,8 +210,13 @@ enum { kWhole = 0, kRows = 1, kEven = 2, kOdd = 3 };
 // for the wave, and heads fill the registers' dims.  kRows: the same pages, heads
 // of at least a 16-byte chunk.  kEven: any page size.  kOdd: any heads as well.
 
-// Workgroups that a CU's registers hold.
-constexpr int resident(int dp, int ht) { return dp * ht <= 64 ? 3 : dp * ht <= 128 ? 2 : 1; }
+// Waves of a workgroup: as many as a CU's registers hold, so that each CU has one
+// workgroup.  Of two workgroups on a CU one is served before the other: with
+// equal shares of one row of 131072 keys they ended after 28 and 49 us.
+constexpr int waves_of(int dp, int ht, int mode)
+{
+    return dp * ht <= 64 && mode == kWhole ? 16 : dp * ht <= 128 ? 8 : 4;
+}
 
 // The chunk at dim d of a row of few dims, one value at a time, zeros behind it.
 template <int DT>
@@ -289,8 +311,9 @@ __device__ inline float lse_of(float t, float l)
 // wait for keys leaves the values behind them in flight, and the other way
 // round; at a share's end they fetch its last tile again, from the caches.
 template <int DT, int DP, int HT, int MODE>
-__global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
+__global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendArgs a)
 {
+    constexpr int NW = waves_of(DP, HT, MODE);
     constexpr bool kBf16 = DT == MP_BF16, kUni = MODE == kWhole || MODE == kRows;
     constexpr int es = Fmt<DT>::esize, V = Fmt<DT>::V;
     constexpr int KG = kBf16 ? 2 : 1, KT = 16 * KG;  // groups of 16 keys, keys of a tile
@@ -300,15 +323,22 @@ __global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
     constexpr int WB = W * es;                       // their bytes, 8 or 16
     constexpr int PD = DP + 4;                       // a head's outputs in LDS, off the banks of the next head's
 
-    __shared__ float sm[4][16 * HT], sl[4][16 * HT];
-    __shared__ float4 so[4 * 16 * HT * PD / 4];
+    __shared__ float sm[NW][16 * HT], sl[NW][16 * HT];
+    __shared__ float4 so[NW * 16 * HT * PD / 4];
 
     const int tid = threadIdx.x, lane = tid & 63, m = lane & 15, g = lane >> 4;
     const int wave = uniform(tid >> 6);
-    const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group), sets = (uint32_t)a.head_sets;
-    const int step = a.split_waves, wt = 4 / step;  // head tiles of a workgroup
-    // the wave's place among those that share its head tile
-    const int mine = wave / step, place = wave % step;
+    const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group);
+
+    Share share{};
+    share.set_tiles = (uint32_t)a.set_tiles;
+    if (a.shares != 0 && !find_share<KT, NW>(a, blockIdx.x, &share))
+        return;
+    // what is the same in all lanes the compiler is told: addresses then are the wave's
+    const int wt = uniform((int)share.set_tiles);
+    // waves that share a head tile, and this one's head tile and place among them
+    const int step = NW / wt, mine = wave / step, place = wave % step;
+    const uint32_t sets = head_tiles / (uint32_t)wt;
 
     // The tiles of one row and head set that a share takes.
     struct Run {
@@ -328,8 +358,7 @@ __global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
         r.n = keys.n;
         const int tile0 = keys.lo / KT + (int)off;
         r.begin = tile0 + place;
-        // no tiles: a row without keys, and a head tile that is not there
-        r.end = set * wt + mine >= head_tiles || keys.n <= keys.lo ? r.begin : tile0 + (int)r.n_tiles;
+        r.end = keys.n <= keys.lo ? r.begin : tile0 + (int)r.n_tiles;  // a row without keys has no tiles
         return r;
     };
     // The run behind r, if `left` tiles of the share lie behind it.
@@ -357,16 +386,12 @@ __global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
         cur = run_of(row, blockIdx.x - (uint32_t)row * sets, 0, 0x7fffffff, range_of(a, row));
         left = cur.n_tiles;
     } else {
-        Share share;
-        if (!find_share<KT>(a, blockIdx.x, &share))
-            return;
-        // the same in all lanes, which the compiler is told: addresses then are the wave's
         per = (uint32_t)uniform((int)share.per);
         left = (uint32_t)uniform((int)(uint32_t)(share.end - share.at));
         const uint64_t in = uniform(share.at - share.row_at);
         const int row = uniform(share.row);
         const Range keys = range_of(a, row);
-        const uint32_t work = max(1, tiles_of<KT>(keys)), set = (uint32_t)(in / work);
+        const uint32_t work = max(1, tiles_of<KT>(keys)), set = (uint32_t)quotient(in, work);
         cur = run_of(row, set, (uint32_t)(in - (uint64_t)set * work), left, keys);
     }
 
@@ -534,9 +559,9 @@ __global__ __launch_bounds__(256, resident(DP, HT)) void k_attend(AttendArgs a)
 
     for (;;) {
         const bool whole = cur.n_tiles == cur.work;
-        if (cur.off == 0 && tid == 0 && a.split != nullptr)
-            a.split[(int64_t)cur.row * sets + cur.set] =
-                make_int2((int)blockIdx.x, whole ? 1 : (int)((before + cur.work - 1) / per) + 1);
+        if (cur.off == 0 && tid < wt && a.split != nullptr)
+            a.split[(int64_t)cur.row * head_tiles + cur.set * wt + tid] =
+                make_int2((int)blockIdx.x, (whole ? 1 : (int)((before + cur.work - 1) / per) + 1) | wt << 16);
 
         f32x4 o[HT][NC * W];
         float top[HT], sum[HT];
@@ -553,7 +578,15 @@ pass:
             for (int j = 0; j < NC * W; ++j)
                 o[h][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
+        // The waves keep step, or those that are served first would leave the
+        // others to end alone: a barrier every kInStep tiles, as many in each wave.
+        int barriers = again ? 0 : (int)(cur.n_tiles / (uint32_t)step / kInStep), until = kInStep;
         for (int tile = cur.begin; tile < cur.end; tile += step) {
+            if (--until == 0 && barriers > 0) {
+                __builtin_amdgcn_s_barrier();
+                --barriers;
+                until = kInStep;
+            }
             if (MODE != kWhole && tile == cur.begin)
 #pragma unroll
                 for (int h = 0; h < HT; ++h)
@@ -687,7 +720,9 @@ pass:
             }
             load_v();
         }
-        const Heads hd = heads_of(min(cur.set * wt + mine, head_tiles - 1));
+        for (; barriers > 0; --barriers)
+            __builtin_amdgcn_s_barrier();
+        const Heads hd = heads_of(cur.set * wt + mine);
         if constexpr (kBf16)
             if (!again) {
                 bool nan = false;
@@ -717,7 +752,7 @@ pass:
 #pragma unroll
             for (int h = 0; h < HT; ++h) {
                 const int head = 16 * h + m;
-                if (cur.set * wt + mine >= head_tiles || head >= hd.nh)
+                if (head >= hd.nh)
                     continue;
                 const float r = sum[h] == 0.0f ? 0.0f : whole ? 1.0f / sum[h] : 1.0f;
                 T* out = static_cast<T*>(a.out) + cur.row * a.ldo + (head0 + head) * a.dim;
@@ -802,35 +837,44 @@ pass:
                     sl[wave][16 * h + m] = all_sum[h];
                 }
             __syncthreads();
-            // The sums of a head tile's waves, by all threads.
-            const float* sof = reinterpret_cast<const float*>(so);
-            for (int w = 0; w < 4; w += step) {
-                const uint32_t tile = cur.set * wt + w / step;
-                if (tile >= head_tiles)
-                    break;
-                const Heads of = heads_of(tile);
-                const int heads = of.nh;
-                const int64_t head0 = (int64_t)of.kvh * a.group + of.gh0, at = (slot + w / step) * a.unit_heads;
-                T* out = static_cast<T*>(a.out) + cur.row * a.ldo + head0 * a.dim;
-                float* part = a.part + at * a.dim;
-                for (int d = tid % DP, h = tid / DP; h < heads; h += 256 / DP)
-                    if (d < a.dim) {
-                        float x = sof[(w * 16 * HT + h) * PD + d];
-                        for (int v = w + 1; v < w + step; ++v)
-                            x += sof[(v * 16 * HT + h) * PD + d];
-                        if (whole) {
-                            const float l = sl[w][h];
-                            out[h * a.dim + d] = (T)(l == 0.0f ? 0.0f : x / l);
-                        } else {
-                            part[h * a.dim + d] = x;
-                        }
+            // The sums of each head tile's waves, by all threads, four dims each.
+            constexpr int D4 = DP / 4;
+            for (int i = tid / D4, d = tid % D4 * 4; i < wt * a.unit_heads; i += 64 * NW / D4) {
+                const int t = (int)a.by_heads.of((uint32_t)i), h = i - t * a.unit_heads;
+                const Heads of = heads_of(cur.set * wt + t);
+                if (h >= of.nh || d >= a.dim)
+                    continue;
+                const int w = t * step;  // the tile's first wave
+                float4 x = so[((w * 16 * HT + h) * PD + d) / 4];
+                for (int v = w + 1; v < w + step; ++v) {
+                    const float4 y = so[((v * 16 * HT + h) * PD + d) / 4];
+                    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+                }
+                const float l = sl[w][h];
+                const int64_t head = (int64_t)of.kvh * a.group + of.gh0 + h, at = (slot + t) * a.unit_heads + h;
+                if (whole) {
+                    const float r = l == 0.0f ? 0.0f : 1.0f / l;
+                    const float f[4] = {l == 0.0f ? 0.0f : x.x * r, l == 0.0f ? 0.0f : x.y * r,
+                                        l == 0.0f ? 0.0f : x.z * r, l == 0.0f ? 0.0f : x.w * r};
+                    T* out = static_cast<T*>(a.out) + cur.row * a.ldo + head * a.dim + d;
+                    if (d + 4 <= a.dim)
+                        st_dims<DT, 4>(out, f);
+                    else
+                        for (int k = 0; d + k < a.dim; ++k)
+                            out[k] = (T)f[k];
+                    if (d == 0 && a.lse != nullptr)
+                        a.lse[cur.row * (int64_t)(a.heads * a.group) + head] = lse_of(sm[w][h], l);
+                } else {
+                    float* part = a.part + at * a.dim + d;
+                    if (a.dim % 4 == 0) {
+                        *reinterpret_cast<float4*>(part) = x;
+                    } else {
+                        const float f[4] = {x.x, x.y, x.z, x.w};
+                        for (int k = 0; k < 4 && d + k < a.dim; ++k)
+                            part[k] = f[k];
                     }
-                if (tid < heads) {
-                    const float t = sm[w][tid], l = sl[w][tid];
-                    if (!whole)
-                        a.stat[at + tid] = make_float2(t, l);
-                    else if (a.lse != nullptr)
-                        a.lse[cur.row * (int64_t)(a.heads * a.group) + head0 + tid] = lse_of(t, l);
+                    if (d == 0)
+                        a.stat[at] = make_float2(sm[w][h], l);
                 }
             }
             __syncthreads();  // LDS is read
@@ -843,96 +887,98 @@ pass:
     }
 }
 
-// Joins the parts of a row: their sums relative to the largest of their maxima.
-// A workgroup takes 4 `lanes` dims of one query head, a float4 a thread, the
-// other threads further parts.
-template <int DT>
-__global__ __launch_bounds__(256) void k_join(AttendArgs a, int lanes)
+// Joins the parts of a row, at most kShares: their sums relative to the largest
+// of their maxima.  A workgroup takes 4 LANES dims of one query head, a float4 a
+// thread, the other threads further parts; what a thread adds first is on its
+// way while the statistics come in.
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void k_join(AttendArgs a)
 {
+    constexpr int kGroups = 256 / LANES, kFirst = 4;
     const uint32_t heads = (uint32_t)(a.heads * a.group);
     const int row = (int)(blockIdx.x / heads), head = (int)(blockIdx.x - (uint32_t)row * heads);
     const int kvh = head / a.group, gh = head - kvh * a.group;
-    const int ht = kvh * a.tiles_of_group + gh / a.unit_heads, wt = 4 / a.split_waves;
-    const int2 split = a.split[(int64_t)row * a.head_sets + ht / wt];
-    const int n = split.y;
+    const int ht = kvh * a.tiles_of_group + gh / a.unit_heads;
+    const int2 split = a.split[(int64_t)row * (a.heads * a.tiles_of_group) + ht];
+    const int n = split.y & 0xffff, wt = split.y >> 16;
     if (n <= 1)
         return;
-    __shared__ float weight[kMostShares];
+    __shared__ float weight[kShares];
     __shared__ float tmp[8];
-    __shared__ float4 acc[256];
-    const int tid = threadIdx.x;
+    __shared__ float4 acc[4][LANES];
+    const int tid = threadIdx.x, wave = tid >> 6, mine = tid / LANES, d = (int)(blockIdx.y * LANES + tid % LANES) * 4;
     // part c of the row, in the first place of a share but for part 0
     const auto place = [&](int c) {
         return ((2 * (int64_t)(split.x + c) + (c == 0 ? 1 : 0)) * wt + ht % wt) * a.unit_heads + gh % a.unit_heads;
     };
-    float t = -INFINITY;
-    for (int c = tid; c < n; c += 256)
-        t = fmaxf(t, a.stat[place(c)].x);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        t = fmaxf(t, __shfl_xor(t, o));
-    if ((tid & 63) == 0)
-        tmp[tid >> 6] = t;
-    __syncthreads();
-    t = fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
-    const float zero = t == -INFINITY ? 0.0f : t;
-    float l = 0.0f;
-    for (int c = tid; c < n; c += 256) {
-        const float2 s = a.stat[place(c)];
-        const float w = __builtin_amdgcn_exp2f(s.x - zero);
-        weight[c] = w;
-        l += s.y * w;
-    }
-    l = wave_xor_sum(l);
-    if ((tid & 63) == 0)
-        tmp[4 + (tid >> 6)] = l;
-    __syncthreads();
-    l = tmp[4] + tmp[5] + tmp[6] + tmp[7];
-    const int groups = 256 / lanes, mine = tid / lanes, d = (int)(blockIdx.y * lanes + tid % lanes) * 4;
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const auto add = [&](float4 v, float w) {
-        sum.x += v.x * w;
-        sum.y += v.y * w;
-        sum.z += v.z * w;
-        sum.w += v.w * w;
-    };
     const auto part = [&](int c) {
         const float* q = a.part + place(c) * a.dim + d;
+        if (c >= n || d >= a.dim)
+            return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (a.dim % 4 == 0)
             return *reinterpret_cast<const float4*>(q);
         const int k = a.dim - d;
         return make_float4(q[0], k > 1 ? q[1] : 0.0f, k > 2 ? q[2] : 0.0f, k > 3 ? q[3] : 0.0f);
     };
-    if (d < a.dim) {
-        int c = mine;
-        for (; c + 3 * groups < n; c += 4 * groups) {
-            const float4 v0 = part(c), v1 = part(c + groups), v2 = part(c + 2 * groups), v3 = part(c + 3 * groups);
-            add(v0, weight[c]);
-            add(v1, weight[c + groups]);
-            add(v2, weight[c + 2 * groups]);
-            add(v3, weight[c + 3 * groups]);
-        }
-        for (; c < n; c += groups)
-            add(part(c), weight[c]);
-    }
-    acc[tid] = sum;
-    // halves onto halves; the number of groups is a power of two
-    for (int k = groups / 2; k > 0; k /= 2) {
-        __syncthreads();
-        if (mine < k) {
-            const float4 v = acc[tid + k * lanes];
-            add(v, 1.0f);
-            acc[tid] = sum;
-        }
-    }
-    using T = typename Elem<DT>::T;
-    if (mine == 0 && d < a.dim) {
-        T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.dim + d;
-        const float x[4] = {sum.x, sum.y, sum.z, sum.w};
+    const float2 s = tid < n ? a.stat[place(tid)] : make_float2(-INFINITY, 0.0f);
+    float4 v[kFirst];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (d + j < a.dim)
-                out[j] = (T)(l == 0.0f ? 0.0f : x[j] / l);
+    for (int i = 0; i < kFirst; ++i)
+        v[i] = part(mine + i * kGroups);
+    float t = s.x;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        t = fmaxf(t, __shfl_xor(t, o));
+    if ((tid & 63) == 0)
+        tmp[wave] = t;
+    __syncthreads();
+    t = fmaxf(fmaxf(tmp[0], tmp[1]), fmaxf(tmp[2], tmp[3]));
+    const float w = __builtin_amdgcn_exp2f(s.x - (t == -INFINITY ? 0.0f : t));
+    weight[tid] = w;
+    float l = wave_xor_sum(s.y * w);
+    if ((tid & 63) == 0)
+        tmp[4 + wave] = l;
+    __syncthreads();
+    l = tmp[4] + tmp[5] + tmp[6] + tmp[7];
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const auto add = [&](float4 p, float f) {
+        x[0] += p.x * f;
+        x[1] += p.y * f;
+        x[2] += p.z * f;
+        x[3] += p.w * f;
+    };
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i)
+        if (mine + i * kGroups < n)
+            add(v[i], weight[mine + i * kGroups]);
+    for (int c = mine + kFirst * kGroups; c < n; c += kFirst * kGroups) {
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i)
+            v[i] = part(c + i * kGroups);
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i)
+            if (c + i * kGroups < n)
+                add(v[i], weight[c + i * kGroups]);
+    }
+    // over the groups of a wave, then over the waves
+#pragma unroll
+    for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            x[k] += __shfl_xor(x[k], o);
+    if ((tid & 63) < LANES)
+        acc[wave][tid % LANES] = make_float4(x[0], x[1], x[2], x[3]);
+    __syncthreads();
+    if (tid < LANES && d < a.dim) {
+        using T = typename Elem<DT>::T;
+        const float4 p0 = acc[0][tid], p1 = acc[1][tid], p2 = acc[2][tid], p3 = acc[3][tid];
+        const float y[4] = {p0.x + p1.x + p2.x + p3.x, p0.y + p1.y + p2.y + p3.y, p0.z + p1.z + p2.z + p3.z,
+                            p0.w + p1.w + p2.w + p3.w};
+        T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.dim + d;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (d + k < a.dim)
+                out[k] = (T)(l == 0.0f ? 0.0f : y[k] / l);
     }
     if (a.lse != nullptr && tid == 0 && blockIdx.y == 0)
         a.lse[(int64_t)row * heads + head] = lse_of(t, l);
@@ -940,72 +986,80 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a, int lanes)
 
 // ---------------------------------------------------------------- the host's side
 struct Plan {
-    int ht = 1, split_waves = 4;
-    int64_t head_tiles = 1, sets = 1, unit_heads = 1;
+    int dp = 64, ht = 1, mode = kWhole;
+    int64_t head_tiles = 1, set_tiles = 1, unit_heads = 1;
+    bool one_if_few = false;
     int64_t shares = 0;  // 0: no row is split
 };
-
-int split_waves_of(int64_t rows, int64_t head_tiles)
-{
-    return rows * head_tiles < 256 ? 4 : head_tiles % 4 == 0 ? 1 : head_tiles % 2 == 0 ? 2 : 4;
-}
 
 Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
 {
     Plan p;
+    const int V = c.dtype == MP_F32 ? 4 : 8, dim = (int)c.head_dim;
     const int64_t group = s.q_heads / c.heads, tile = c.dtype == MP_F32 ? 16 : 32;
-    p.ht = group > 16 && c.head_dim <= 128 ? 2 : 1;
+    p.dp = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+    p.mode = dim < V ? kOdd : c.page_size % 16 != 0 ? kEven : dim == p.dp ? kWhole : kRows;
+    p.ht = group > 16 && dim <= 128 ? 2 : 1;
     p.head_tiles = c.heads * ((group + 16 * p.ht - 1) / (16 * p.ht));
     p.unit_heads = std::min<int64_t>(group, 16 * p.ht);
-    p.split_waves = split_waves_of(s.rows, p.head_tiles);
-    const int64_t wt = 4 / p.split_waves;
-    p.sets = (p.head_tiles + wt - 1) / wt;
+    while (p.set_tiles < waves_of(p.dp, p.ht, p.mode) && p.head_tiles % (2 * p.set_tiles) == 0)
+        p.set_tiles *= 2;
+    p.one_if_few = s.rows * p.head_tiles < kShares;
     int64_t most = s.width * c.page_size;
     const bool slides = s.window > 0 && s.window < most;
     most = slides ? s.window : most;
     const int64_t tiles = (most + tile - 1) / tile + (slides ? 1 : 0);  // a window may begin inside a tile
-    if (tiles > kMinTiles) {
-        const int64_t needed = (s.rows * p.sets * tiles + kMinTiles - 1) / kMinTiles;  // < 2^50
-        const int dp = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
-        p.shares = std::min<int64_t>(256 * resident(dp, p.ht), needed);
-    }
+    if (tiles > kMinTiles)
+        p.shares = std::min<int64_t>(kShares, (s.rows * p.head_tiles * tiles + kMinTiles - 1) / kMinTiles);
+    else if (p.one_if_few)
+        p.set_tiles = 1;
     return p;
 }
 
 uint64_t up16(uint64_t n) { return (n + 15) / 16 * 16; }
-// query heads of all parts: two of a share, of 4 / split_waves head tiles
-uint64_t slot_heads(const Plan& p) { return (uint64_t)(2 * p.shares * (4 / p.split_waves) * p.unit_heads); }
+// query heads of all parts: two of a share
+uint64_t slot_heads(const Plan& p) { return (uint64_t)(2 * p.shares * p.set_tiles * p.unit_heads); }
+
+template <int DT, int DP, int HT, int MODE>
+void launch_mode(const AttendArgs& a, unsigned grid, hipStream_t st)
+{
+    k_attend<DT, DP, HT, MODE><<<grid, 64 * waves_of(DP, HT, MODE), 0, st>>>(a);
+}
 
 template <int DT, int DP, int HT>
 void launch_tiles(const AttendArgs& a, unsigned grid, int mode, hipStream_t st)
 {
     if (mode == kWhole)
-        k_attend<DT, DP, HT, kWhole><<<grid, 256, 0, st>>>(a);
+        launch_mode<DT, DP, HT, kWhole>(a, grid, st);
     else if (mode == kRows)
-        k_attend<DT, DP, HT, kRows><<<grid, 256, 0, st>>>(a);
+        launch_mode<DT, DP, HT, kRows>(a, grid, st);
     else if (mode == kEven)
-        k_attend<DT, DP, HT, kEven><<<grid, 256, 0, st>>>(a);
+        launch_mode<DT, DP, HT, kEven>(a, grid, st);
     else if constexpr (DP == 64)
-        k_attend<DT, DP, HT, kOdd><<<grid, 256, 0, st>>>(a);
+        launch_mode<DT, DP, HT, kOdd>(a, grid, st);
 }
 
 template <int DT>
 void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
 {
-    const int dp = a.dim <= 64 ? 64 : a.dim <= 128 ? 128 : 256;
-    const int mode = a.dim < Fmt<DT>::V ? kOdd : a.page_size % 16 != 0 ? kEven : a.dim == dp ? kWhole : kRows;
-    const unsigned grid = (unsigned)(p.shares ? p.shares : a.rows * p.sets);
-    if (dp == 64)
-        p.ht == 2 ? launch_tiles<DT, 64, 2>(a, grid, mode, st) : launch_tiles<DT, 64, 1>(a, grid, mode, st);
-    else if (dp == 128)
-        p.ht == 2 ? launch_tiles<DT, 128, 2>(a, grid, mode, st) : launch_tiles<DT, 128, 1>(a, grid, mode, st);
+    const unsigned grid = (unsigned)(p.shares ? p.shares : a.rows * (p.head_tiles / p.set_tiles));
+    if (p.dp == 64)
+        p.ht == 2 ? launch_tiles<DT, 64, 2>(a, grid, p.mode, st) : launch_tiles<DT, 64, 1>(a, grid, p.mode, st);
+    else if (p.dp == 128)
+        p.ht == 2 ? launch_tiles<DT, 128, 2>(a, grid, p.mode, st) : launch_tiles<DT, 128, 1>(a, grid, p.mode, st);
     else
-        launch_tiles<DT, 256, 1>(a, grid, mode, st);
+        launch_tiles<DT, 256, 1>(a, grid, p.mode, st);
     if (p.shares) {
         // few heads: their dims in slices of 32, so that more workgroups share the parts
         const unsigned heads = (unsigned)(a.rows * a.heads * a.group);
-        const int lanes = heads < 512 ? 8 : dp / 4;
-        k_join<DT><<<dim3(heads, (unsigned)((a.dim + 4 * lanes - 1) / (4 * lanes))), 256, 0, st>>>(a, lanes);
+        if (heads < 512)
+            k_join<DT, 8><<<dim3(heads, (unsigned)((a.dim + 31) / 32)), 256, 0, st>>>(a);
+        else if (p.dp == 64)
+            k_join<DT, 16><<<heads, 256, 0, st>>>(a);
+        else if (p.dp == 128)
+            k_join<DT, 32><<<heads, 256, 0, st>>>(a);
+        else
+            k_join<DT, 64><<<heads, 256, 0, st>>>(a);
     }
 }
 
@@ -1016,7 +1070,7 @@ uint64_t kv_attend_ws_bytes(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     const Plan p = plan_of(c, s);
     if (s.rows == 0 || p.shares == 0)
         return 0;
-    return up16((uint64_t)(s.rows * p.sets) * sizeof(int2)) + up16(slot_heads(p) * sizeof(float2)) +
+    return up16((uint64_t)(s.rows * p.head_tiles) * sizeof(int2)) + up16(slot_heads(p) * sizeof(float2)) +
            slot_heads(p) * (uint64_t)c.head_dim * sizeof(float);
 }
 
@@ -1035,7 +1089,7 @@ hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, c
     if (p.shares) {
         char* w = static_cast<char*>(ws);
         a.split = reinterpret_cast<int2*>(w);
-        w += up16((uint64_t)(s.rows * p.sets) * sizeof(int2));
+        w += up16((uint64_t)(s.rows * p.head_tiles) * sizeof(int2));
         a.stat = reinterpret_cast<float2*>(w);
         w += up16(slot_heads(p) * sizeof(float2));
         a.part = reinterpret_cast<float*>(w);
@@ -1055,12 +1109,13 @@ hipError_t launch_kv_attend(const mp_kv_cache& c, const mp_kv_attend_shape& s, c
     a.group = (int32_t)(s.q_heads / c.heads);
     a.dim = (int32_t)c.head_dim;
     a.tiles_of_group = (int32_t)(p.head_tiles / c.heads);
-    a.split_waves = p.split_waves;
-    a.head_sets = (int32_t)p.sets;
+    a.set_tiles = (int32_t)p.set_tiles;
+    a.one_if_few = p.one_if_few;
     a.shares = (int32_t)p.shares;
     a.unit_heads = (int32_t)p.unit_heads;
     a.by_page = Div((uint32_t)c.page_size);
     a.by_tiles = Div((uint32_t)a.tiles_of_group);
+    a.by_heads = Div((uint32_t)p.unit_heads);
     a.scale = (float)((double)s.scale * 1.4426950408889634);
     if (c.dtype == MP_F32)
         launch_type<MP_F32>(a, p, st);
