@@ -102,10 +102,14 @@ __device__ inline uint32_t work_of(const AttendArgs& a, int row)
 // The call's tiles are the sequence (row, head set, tile), and a share is a run
 // of it, of `per` tiles from `at` on; it begins in `row`, whose first tile is at
 // row_at.
+// Where the tiles are few, a run is instead one of the equal parts of a row and
+// head set, so that no share holds two: 7 rows of up to 2000 fp32 keys 25.2 us
+// cut evenly, 21.5 so.
 struct Share {
     uint64_t at, end, row_at;
     uint32_t per, set_tiles;
     int row;
+    uint32_t parts;  // of the row and head set; 0: as `per` says
 };
 
 // Inclusive sum over the lanes before, and its own.
@@ -164,7 +168,8 @@ __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* o
     // which counts below two tiles a wave: one row of 4096 keys 14.6 and 17.7 us,
     // of 32768 23.6 and 23.6, of 131072 59 and 55.
     const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group);
-    out->set_tiles = a.one_if_few && total * head_tiles < 2 * kShares * NW ? 1 : (uint32_t)a.set_tiles;
+    const bool few = total * head_tiles < 2 * kShares * NW;
+    out->set_tiles = a.one_if_few && few ? 1 : (uint32_t)a.set_tiles;
     const uint32_t sets = head_tiles / out->set_tiles;
     const uint64_t all = total * sets, even = quotient(all + a.shares - 1, (uint32_t)a.shares);
     out->per = even < kMinTiles ? (uint32_t)kMinTiles : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
@@ -172,6 +177,45 @@ __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* o
     out->end = min(all, out->at + out->per);
     out->row = 0;
     out->row_at = 0;
+    out->parts = 0;
+    const uint32_t runs = (uint32_t)a.rows * sets;
+    if (few && 4 * runs <= (uint32_t)a.shares) {
+        // all / C + runs parts of at most C tiles: no more than the shares
+        const uint32_t room = (uint32_t)a.shares - runs;
+        const uint32_t C = max((uint32_t)kMinTiles, ((uint32_t)all + room - 1) / room);
+        const auto take = [&](int row, uint32_t before, uint32_t work, uint32_t row_at) {
+            // the part `number` among this row's, counted from `before` on
+            const uint32_t parts = (work + C - 1) / C, in = number - before, set = in / parts, j = in - set * parts;
+            out->row = row;
+            out->row_at = row_at;
+            out->parts = parts;
+            out->at = row_at + (uint64_t)set * work + work * j / parts;
+            out->end = row_at + (uint64_t)set * work + work * (j + 1) / parts;
+        };
+        if (a.rows == 1) {
+            if (number >= ((uint32_t)total + C - 1) / C * sets)
+                return false;
+            take(0, 0, (uint32_t)total, 0);
+            return true;
+        }
+        // the rows are those of the first wave's lanes
+        __shared__ uint32_t found[3];
+        const uint32_t parts = (own + C - 1) / C * sets, before = wave_scan(parts) - parts;
+        if (tid == 0)
+            found_row = -1;
+        __syncthreads();
+        if (wave == 0 && number >= before && number - before < parts) {
+            found_row = tid;
+            found[0] = before;
+            found[1] = own;
+            found[2] = (uint32_t)mine * sets;
+        }
+        __syncthreads();
+        if (found_row < 0)
+            return false;
+        take(found_row, found[0], found[1], found[2]);
+        return true;
+    }
     if (out->at >= all)
         return false;
     if (a.rows == 1)
@@ -381,12 +425,14 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
 
     Run cur;
     uint32_t left, before = 0, per = 0;  // tiles of the share from cur on, and before it; tiles of a share
+    int parts = 0;                       // of the run's row and head set, where that is known
     if (a.shares == 0) {
         const int row = (int)(blockIdx.x / sets);
         cur = run_of(row, blockIdx.x - (uint32_t)row * sets, 0, 0x7fffffff, range_of(a, row));
         left = cur.n_tiles;
     } else {
         per = (uint32_t)uniform((int)share.per);
+        parts = uniform((int)share.parts);
         left = (uint32_t)uniform((int)(uint32_t)(share.end - share.at));
         const uint64_t in = uniform(share.at - share.row_at);
         const int row = uniform(share.row);
@@ -561,7 +607,7 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
         const bool whole = cur.n_tiles == cur.work;
         if (cur.off == 0 && tid < wt && a.split != nullptr)
             a.split[(int64_t)cur.row * head_tiles + cur.set * wt + tid] =
-                make_int2((int)blockIdx.x, (whole ? 1 : (int)((before + cur.work - 1) / per) + 1) | wt << 16);
+                make_int2((int)blockIdx.x, (whole ? 1 : parts ? parts : (int)((before + cur.work - 1) / per) + 1) | wt << 16);
 
         f32x4 o[HT][NC * W];
         float top[HT], sum[HT];

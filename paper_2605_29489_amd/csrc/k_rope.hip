@@ -36,6 +36,16 @@ struct Div {
     __device__ inline uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
 };
 
+// Outputs are written once and are more than the caches hold where it counts:
+// rotations of 16384 x 32 x 128 bf16 59.8 us with plain stores and 53.3 with
+// non-temporal ones, of 8192 x 40 x 128 39.0 and 28.6.  Non-temporal loads as
+// well: 51.1 and 33.3.
+__device__ inline void st16n(void* p, uint4 c)
+{
+    const u32x4_t v = {c.x, c.y, c.z, c.w};
+    __builtin_nontemporal_store(v, static_cast<u32x4_a2*>(p));
+}
+
 // What one launch turns and copies.  A token's work is a row of items: those of
 // its x heads (turned into y), then, with a cache, of its keys (turned) and its
 // values (copied).  An item is a 16-byte chunk of a head, or, where pairs lie
@@ -46,7 +56,7 @@ struct TurnArgs {
     int tw;             // tokens of a workgroup
     int dim, rot, per;  // items of a turned head
     uint32_t nx, nk, all;  // items of a token: x's, and keys', and all
-    Div by_all, by_per, by_copy;
+    Div by_all, by_per, by_copy, by_page;
     const int64_t* pos;
     const double* freqs;
     float amplitude, sign;
@@ -62,14 +72,19 @@ struct TurnArgs {
     void* cv;
 };
 
-constexpr int kItems = 4;           // of a thread, loaded together
+constexpr int kThreads = 256;
 constexpr int64_t kMaxTurns = 4096;  // cos and sin pairs of a workgroup: 32 KB of LDS
 
 // Bound by memory, and where there are few tokens by one launch and one trip to
-// memory: a workgroup's first items are on their way while the cos and sin of
-// its tokens, one pair a thread, are formed and shared through LDS by all heads.
+// memory: a workgroup's first items, one a thread, are on their way while the
+// cos and sin of its tokens, one pair a thread, are formed and shared through LDS
+// by all heads.  One item at a time keeps reads and writes close together: with
+// 1, 2, 4 and 8 of them 16384 x 32 x 128 bf16 take 47.7, 49.3, 53.5 and 65 us (a
+// copy 42), 8192 x 40 x 128 26.9, 28.7, 29.1 and 40 (a copy 28).  With a token's
+// items in equal parts, each in a workgroup of its own, 47.0 and 27.5, and appends
+// of 8192 tokens with 32 + 8 + 8 heads 47.8 for 41.0.
 template <int DT, bool INTER, bool VEC, bool APPEND>
-__global__ __launch_bounds__(256) void k_turn(TurnArgs a)
+__global__ __launch_bounds__(kThreads) void k_turn(TurnArgs a)
 {
     using T = typename Elem<DT>::T;
     constexpr int V = VEC ? Fmt<DT>::V : 1;
@@ -77,158 +92,135 @@ __global__ __launch_bounds__(256) void k_turn(TurnArgs a)
     const int half = a.rot / 2, tid = threadIdx.x;
     int64_t* place = reinterpret_cast<int64_t*>(turns + a.tw * half);
     const uint32_t turned = (uint32_t)(INTER ? a.rot / (VEC ? V : 2) : half / V);  // turned items of a head
-
-    struct Item {
-        uint32_t t, h, j;  // token, head and item of the head; kind: 0 x, 1 key, 2 value, 3 none
-        uint32_t kind;
-        uint4 lo, hi;
-    };
-    Item it[kItems];
+    enum { kX, kKey, kValue };
 
     for (int64_t t0 = (int64_t)blockIdx.x * a.tw; t0 < a.tokens; t0 += (int64_t)gridDim.x * a.tw) {
         const int nt = (int)(a.tokens - t0 < a.tw ? a.tokens - t0 : a.tw);
-        const uint32_t n = (uint32_t)nt * a.all;
-        // elements of an item: VEC chunks at [off] (and [off + half]), else single values
-        auto offset = [&](const Item& i) -> int {
-            if (APPEND && i.kind == 2)
-                return (int)i.j * V;
-            if constexpr (VEC)
-                return INTER || i.j < turned ? (int)i.j * V : (int)(i.j - turned) * V + a.rot;
+        const uint32_t end = (uint32_t)nt * a.all;
+        // this thread's item: of token t and head h, number j; VEC chunks at `off` (and off + half), else values
+        uint32_t t = 0, h = 0, j = 0;
+        int kind = kX, off = 0;
+        bool pair = false;
+        uint4 lo{}, hi{};
+        const auto load = [&](uint32_t at) {
+            t = a.by_all.of(at);
+            uint32_t r = at - t * a.all;
+            const T* p;
+            if (!APPEND || r < a.nx) {
+                kind = kX;
+                h = a.by_per.of(r);
+                j = r - h * a.per;
+                p = static_cast<const T*>(a.x) + (t0 + t) * a.ldx + h * a.hdx;
+            } else if (r < a.nk) {
+                r -= a.nx;
+                kind = kKey;
+                h = a.by_per.of(r);
+                j = r - h * a.per;
+                p = static_cast<const T*>(a.k) + (t0 + t) * a.ldk + (int64_t)h * a.dim;
+            } else {
+                r -= a.nk;
+                kind = kValue;
+                h = a.by_copy.of(r);
+                j = r - h * a.by_copy.d;
+                p = static_cast<const T*>(a.v) + (t0 + t) * a.ldv + (int64_t)h * a.dim;
+            }
+            pair = kind != kValue && j < turned;
+            if (kind == kValue || (VEC && INTER))
+                off = (int)j * V;
+            else if (pair)
+                off = (int)j * (INTER ? 2 : V);
             else
-                return i.j >= turned ? (int)(i.j - turned) + a.rot : INTER ? 2 * (int)i.j : (int)i.j;
-        };
-        auto load = [&](uint32_t base) {
-#pragma unroll
-            for (int u = 0; u < kItems; ++u) {
-                Item& i = it[u];
-                const uint32_t at = base + u * 256 + tid;
-                i.kind = 3;
-                if (at >= n)
-                    continue;
-                i.t = a.by_all.of(at);
-                uint32_t r = at - i.t * a.all;
-                const T* p;
-                if (!APPEND || r < a.nx) {
-                    i.kind = 0;
-                    i.h = a.by_per.of(r);
-                    i.j = r - i.h * a.per;
-                    p = static_cast<const T*>(a.x) + (t0 + i.t) * a.ldx + i.h * a.hdx;
-                } else if (r < a.nk) {
-                    r -= a.nx;
-                    i.kind = 1;
-                    i.h = a.by_per.of(r);
-                    i.j = r - i.h * a.per;
-                    p = static_cast<const T*>(a.k) + (t0 + i.t) * a.ldk + (int64_t)i.h * a.dim;
-                } else {
-                    r -= a.nk;
-                    i.kind = 2;
-                    i.h = a.by_copy.of(r);
-                    i.j = r - i.h * a.by_copy.d;
-                    p = static_cast<const T*>(a.v) + (t0 + i.t) * a.ldv + (int64_t)i.h * a.dim;
-                }
-                p += offset(i);
-                const bool pair = i.kind != 2 && i.j < turned;
-                if constexpr (VEC) {
-                    i.lo = ld16u(p);
-                    if (!INTER && pair)
-                        i.hi = ld16u(p + half);
-                } else {
-                    const auto bits = [](const T* q) -> uint32_t {
-                        if constexpr (DT == MP_F32)
-                            return *reinterpret_cast<const uint32_t*>(q);
-                        else
-                            return *reinterpret_cast<const uint16_t*>(q);
-                    };
-                    i.lo.x = bits(p);
-                    if (pair)
-                        i.hi.x = bits(p + (INTER ? 1 : half));
-                }
+                off = (int)(j - turned) * V + a.rot;
+            p += off;
+            if constexpr (VEC) {
+                lo = ld16u(p);
+                if (!INTER && pair)
+                    hi = ld16u(p + half);
+            } else {
+                const auto bits = [](const T* q) -> uint32_t {
+                    if constexpr (DT == MP_F32)
+                        return *reinterpret_cast<const uint32_t*>(q);
+                    else
+                        return *reinterpret_cast<const uint16_t*>(q);
+                };
+                lo.x = bits(p);
+                if (pair)
+                    hi.x = bits(p + (INTER ? 1 : half));
             }
         };
-        load(0);
+        if (tid < end)
+            load(tid);
         if (t0 != (int64_t)blockIdx.x * a.tw)
-            __syncthreads();  // the group before is done with the turns
-        for (int i = tid; i < nt * half; i += 256) {
-            const int t = i / half;
-            float2 w = turn_of(a.pos[t0 + t], a.freqs[i - t * half], a.amplitude);
+            __syncthreads();  // the tokens before are done with the turns
+        for (int i = tid; i < nt * half; i += kThreads) {
+            const int u = i / half;
+            float2 w = turn_of(a.pos[t0 + u], a.freqs[i - u * half], a.amplitude);
             w.y *= a.sign;
             turns[i] = w;
         }
         if constexpr (APPEND)
-            for (int t = tid; t < nt; t += 256) {
-                const int64_t slot = a.slots[t0 + t];
+            for (int u = tid; u < nt; u += kThreads) {
+                const int64_t slot = a.slots[t0 + u];
                 const bool in = slot >= 0 && slot < a.pages * a.page_size;
-                const int64_t page = in ? slot / a.page_size : 0;
-                place[t] = in ? page * a.page_stride + (slot - page * a.page_size) * a.slot_stride : -1;
+                const int64_t page = !in ? 0 : slot >> 31 ? slot / a.page_size : a.by_page.of((uint32_t)slot);
+                place[u] = in ? page * a.page_stride + (slot - page * a.page_size) * a.slot_stride : -1;
             }
         __syncthreads();
-        for (uint32_t base = 0;;) {
-#pragma unroll
-            for (int u = 0; u < kItems; ++u) {
-                Item& i = it[u];
-                if (i.kind == 3)
-                    continue;
-                T* p;
-                if (!APPEND || i.kind == 0) {
-                    p = static_cast<T*>(a.y) + (t0 + i.t) * a.ldy + i.h * a.hdy;
-                } else {
-                    const int64_t at = place[i.t];
-                    if (at < 0)
-                        continue;
-                    p = static_cast<T*>(i.kind == 1 ? a.ck : a.cv) + at + i.h * a.head_stride;
-                }
-                p += offset(i);
-                const bool pair = i.kind != 2 && i.j < turned;
-                const float2* w = turns + i.t * half + (pair ? i.j * (INTER && VEC ? V / 2 : V) : 0);
-                if constexpr (VEC) {
-                    if (pair) {
-                        float f[V];
-                        Fmt<DT>::unpack(i.lo, f);
-                        if constexpr (INTER) {
-                            float y[V];
-#pragma unroll
-                            for (int e = 0; e < V; e += 2) {
-                                const float2 c = w[e / 2];
-                                y[e] = f[e] * c.x - f[e + 1] * c.y;
-                                y[e + 1] = f[e] * c.y + f[e + 1] * c.x;
-                            }
-                            i.lo = Fmt<DT>::pack(y);
-                        } else {
-                            float g[V], y[V], z[V];
-                            Fmt<DT>::unpack(i.hi, g);
-#pragma unroll
-                            for (int e = 0; e < V; ++e) {
-                                const float2 c = w[e];
-                                y[e] = f[e] * c.x - g[e] * c.y;
-                                z[e] = f[e] * c.y + g[e] * c.x;
-                            }
-                            i.lo = Fmt<DT>::pack(y);
-                            st16u(p + half, Fmt<DT>::pack(z));
-                        }
-                    }
-                    st16u(p, i.lo);
-                } else {
-                    const auto put = [](T* q, uint32_t b) {
-                        if constexpr (DT == MP_F32)
-                            *reinterpret_cast<uint32_t*>(q) = b;
-                        else
-                            *reinterpret_cast<uint16_t*>(q) = (uint16_t)b;
-                    };
-                    if (pair) {
-                        const float2 c = *w;
-                        constexpr int up = DT == MP_F32 ? 0 : 16;  // a bf16 pattern is the upper half of an fp32 one
-                        const float f = __uint_as_float(i.lo.x << up), g = __uint_as_float(i.hi.x << up);
-                        p[0] = (T)(f * c.x - g * c.y);
-                        p[INTER ? 1 : half] = (T)(f * c.y + g * c.x);
-                    } else {
-                        put(p, i.lo.x);
-                    }
-                }
+        const auto store = [&]() {
+            T* p;
+            if (!APPEND || kind == kX) {
+                p = static_cast<T*>(a.y) + (t0 + t) * a.ldy + h * a.hdy;
+            } else {
+                if (place[t] < 0)
+                    return;
+                p = static_cast<T*>(kind == kKey ? a.ck : a.cv) + place[t] + h * a.head_stride;
             }
-            base += 256 * kItems;
-            if (base >= n)
-                break;
-            load(base);
+            p += off;
+            const float2* w = turns + t * half + (pair ? j * (INTER && VEC ? V / 2 : V) : 0);
+            if constexpr (VEC) {
+                if (pair) {
+                    float f[V];
+                    Fmt<DT>::unpack(lo, f);
+                    if constexpr (INTER) {
+                        float y[V];
+#pragma unroll
+                        for (int e = 0; e < V; e += 2) {
+                            const float2 c = w[e / 2];
+                            y[e] = f[e] * c.x - f[e + 1] * c.y;
+                            y[e + 1] = f[e] * c.y + f[e + 1] * c.x;
+                        }
+                        lo = Fmt<DT>::pack(y);
+                    } else {
+                        float g[V], y[V], z[V];
+                        Fmt<DT>::unpack(hi, g);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const float2 c = w[e];
+                            y[e] = f[e] * c.x - g[e] * c.y;
+                            z[e] = f[e] * c.y + g[e] * c.x;
+                        }
+                        lo = Fmt<DT>::pack(y);
+                        st16n(p + half, Fmt<DT>::pack(z));
+                    }
+                }
+                st16n(p, lo);
+            } else if (pair) {
+                const float2 c = *w;
+                constexpr int up = DT == MP_F32 ? 0 : 16;  // a bf16 pattern is the upper half of an fp32 one
+                const float f = __uint_as_float(lo.x << up), g = __uint_as_float(hi.x << up);
+                p[0] = (T)(f * c.x - g * c.y);
+                p[INTER ? 1 : half] = (T)(f * c.y + g * c.x);
+            } else if constexpr (DT == MP_F32) {
+                *reinterpret_cast<uint32_t*>(p) = lo.x;
+            } else {
+                *reinterpret_cast<uint16_t*>(p) = (uint16_t)lo.x;
+            }
+        };
+        for (uint32_t at = tid; at < end;) {
+            store();
+            at += kThreads;
+            if (at < end)
+                load(at);
         }
     }
 }
@@ -237,9 +229,9 @@ template <int DT, bool INTER, bool VEC>
 void launch_turn(const TurnArgs& a, unsigned grid, size_t lds, bool append, hipStream_t st)
 {
     if (append)
-        k_turn<DT, INTER, VEC, true><<<grid, 256, lds, st>>>(a);
+        k_turn<DT, INTER, VEC, true><<<grid, kThreads, lds, st>>>(a);
     else
-        k_turn<DT, INTER, VEC, false><<<grid, 256, lds, st>>>(a);
+        k_turn<DT, INTER, VEC, false><<<grid, kThreads, lds, st>>>(a);
 }
 
 // heads: turned heads of x; kv: heads of a cache, or 0.
@@ -255,9 +247,8 @@ hipError_t launch(TurnArgs& a, int dtype, bool interleaved, int64_t heads, int64
     a.by_all = Div(a.all);
     a.by_per = Div((uint32_t)a.per);
     a.by_copy = Div((uint32_t)copy);
-    // as many tokens as fill a workgroup's threads with items, fewer where that leaves CUs without a workgroup
-    int64_t tw = std::max<int64_t>(1, 256 * kItems / a.all);
-    tw = std::min(tw, (a.tokens + 511) / 512);
+    // as many tokens as there are threads for, fewer where that leaves CUs without a workgroup
+    int64_t tw = std::min<int64_t>(kThreads / a.all, (a.tokens + 511) / 512);
     tw = std::max<int64_t>(1, std::min(tw, kMaxTurns / std::max(half, 1)));
     a.tw = (int)tw;
     const size_t lds = (size_t)(tw * half) * sizeof(float2) + (size_t)tw * sizeof(int64_t);
@@ -323,6 +314,7 @@ hipError_t launch_kv_append(const mp_kv_cache& c, const mp_kv_rows& r, const voi
     a.slots = slots;
     a.pages = c.pages;
     a.page_size = c.page_size;
+    a.by_page = Div((uint32_t)c.page_size);
     a.page_stride = c.page_stride;
     a.slot_stride = c.slot_stride;
     a.head_stride = c.head_stride;
