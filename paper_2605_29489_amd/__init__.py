@@ -267,7 +267,7 @@ def _stream(stream):
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle alone: 0.3 us against 3
         if raw is not None:
-            return C.c_void_p(raw(torch.cuda.current_device()))
+            return raw(torch.cuda.current_device())
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return C.c_void_p(stream)
@@ -412,13 +412,18 @@ def mp_lora_merge_ties_tau(layout: Layout, base, loras, adapters, mask, tau, lam
 
 
 # ------------------------------------------------------------------ the feed-forward part of a block
-def _dtype_code(t) -> int:
+@functools.lru_cache(maxsize=None)
+def _code_of(dtype) -> int:
     import torch
-    if t.dtype is torch.bfloat16:
+    if dtype is torch.bfloat16:
         return MP_BF16
-    if t.dtype is torch.float32:
+    if dtype is torch.float32:
         return MP_F32
-    raise ValueError(f"dtype {t.dtype} is not torch.float32 or torch.bfloat16")
+    raise ValueError(f"dtype {dtype} is not torch.float32 or torch.bfloat16")
+
+
+def _dtype_code(t) -> int:
+    return _code_of(t.dtype)
 
 
 def _matrix(t, rows, cols, dtype, name: str) -> int:
@@ -623,33 +628,38 @@ def mp_moe_workspace(layer: MoeLayer, dtype: int, tokens: int) -> int:
 
 
 # ------------------------------------------------------------------ attention over a paged cache
-def _heads(t, tokens, heads, dim, dtype, name: str):
-    """Checks tokens x heads x dim values of unit stride inside a head; (token stride, head stride)."""
-    if t.shape != (tokens, heads, dim):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(tokens, heads, dim)}")
+def _heads(t, shape, dtype, name: str):
+    """Checks [tokens, heads, dim] values of unit stride inside a head; (token stride, head stride)."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype is not dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
     st, sh, sd = t.stride()
-    if sd != 1 and dim > 1:
+    if sd != 1 and shape[2] > 1:
         raise ValueError(f"{name}: the values of a head must be adjacent")
     return st, sh
 
 
-def _head_rows(t, tokens, heads, dim, dtype, name: str) -> int:
+def _head_rows(t, shape, dtype, name: str) -> int:
     """The same with the heads of a token side by side; its token stride."""
-    st, sh = _heads(t, tokens, heads, dim, dtype, name)
-    if heads > 1 and sh != dim:
+    st, sh = _heads(t, shape, dtype, name)
+    tokens, heads, dim = shape
+    if sh != dim and heads > 1:
         raise ValueError(f"{name}: the heads of a token must be adjacent")
     return st if tokens > 1 else max(st, heads * dim)
 
 
-def _turn_args(tokens, positions, freqs):
+def _turn_args(tokens, positions, freqs) -> int:
+    """Checks them; the number of turned values of a head."""
+    if freqs is None:
+        return 0
     import torch
+    pairs = freqs.numel()
+    _vector(freqs, pairs, torch.float64, "freqs")
+    if positions is None:
+        raise ValueError("freqs need positions")
     _vector(positions, tokens, torch.int64, "positions")
-    if freqs is not None:
-        _vector(freqs, freqs.numel(), torch.float64, "freqs")
-        if positions is None:
-            raise ValueError("freqs need positions")
+    return 2 * pairs
 
 
 def mp_rope_frequencies(rot_dim: int, base: float = 10000.0, kind: int = MP_ROPE_PLAIN, factor: float = 1.0,
@@ -670,14 +680,13 @@ def mp_rope_frequencies(rot_dim: int, base: float = 10000.0, kind: int = MP_ROPE
 
 
 def _rope(call, x, y, names, positions, freqs, interleaved, amplitude, back, stream):
-    dt = x.dtype
-    T, H, D = x.shape
-    sx, sy = _heads(x, T, H, D, dt, names[0]), _heads(y, T, H, D, dt, names[1])
-    _turn_args(T, positions, freqs)
+    dt, shape = x.dtype, x.shape
+    T, H, D = shape
+    sx, sy = _heads(x, shape, dt, names[0]), _heads(y, shape, dt, names[1])
+    rot = _turn_args(T, positions, freqs)
     if back:
         sx, sy = sy, sx
-    s = mp_rope_shape(_dtype_code(x), MP_ROPE_INTERLEAVED if interleaved else 0, T, H, D, 2 * freqs.numel(), *sx, *sy,
-                      amplitude)
+    s = mp_rope_shape(_code_of(dt), MP_ROPE_INTERLEAVED if interleaved else 0, T, H, D, rot, *sx, *sy, amplitude)
     _check(call(C.byref(s), x.data_ptr(), _ptr(positions), _ptr(freqs), y.data_ptr(), _stream(stream)))
 
 
@@ -701,13 +710,15 @@ class KvCache:
     one array."""
 
     def __init__(self, k, v):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype:
-            raise ValueError(f"k {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}: expected two equal "
+        shape, strides, dt = k.shape, k.stride(), k.dtype
+        if len(shape) != 4 or shape != v.shape or dt is not v.dtype:
+            raise ValueError(f"k {tuple(shape)} {dt}, v {tuple(v.shape)} {v.dtype}: expected two equal "
                              "[pages, page_size, heads, dim]")
-        if k.stride() != v.stride() or (k.stride(3) != 1 and k.shape[3] > 1):
+        if strides != v.stride() or (strides[3] != 1 and shape[3] > 1):
             raise ValueError("k and v need equal strides, and adjacent values in a head")
         self.k, self.v = k, v
-        self._s = mp_kv_cache(_dtype_code(k), 0, *k.shape, *k.stride()[:3], k.data_ptr(), v.data_ptr())
+        self._shape, self._dtype = shape, dt
+        self._s = mp_kv_cache(_code_of(dt), 0, *shape, *strides[:3], k.data_ptr(), v.data_ptr())
         self._ref = C.byref(self._s)
 
 
@@ -718,23 +729,28 @@ def mp_kv_append(cache: KvCache, k, v, slots, positions=None, freqs=None, q=None
     queries ``q`` [tokens, q_heads, dim], turned, in ``q_out`` (default: in place).  Without ``freqs`` nothing is
     turned."""
     import torch
-    dt, (T, H, D) = cache.k.dtype, k.shape
-    ch, cd = cache.k.shape[2:]
-    if (H, D) != (ch, cd):
-        raise ValueError(f"k: {H} heads of {D}, the cache has {ch} of {cd}")
-    ldk, ldv = _head_rows(k, T, H, D, dt, "k"), _head_rows(v, T, H, D, dt, "v")
+    dt, (T, *heads), (_, _, *held) = cache._dtype, k.shape, cache._shape
+    if heads != held:
+        raise ValueError(f"k: heads {heads}, the cache's are {held}")
+    shape = (T, *heads)
+    ldk, ldv = _head_rows(k, shape, dt, "k"), _head_rows(v, shape, dt, "v")
     _vector(slots, T, torch.int64, "slots")
-    _turn_args(T, positions, freqs)
+    rot = _turn_args(T, positions, freqs)
     hq = ldq = ldqo = 0
-    if q is not None:
-        q_out = q if q_out is None else q_out
+    if q is None:
+        q_out = None
+    else:
         hq = q.shape[1]
-        ldq, ldqo = _head_rows(q, T, hq, D, dt, "q"), _head_rows(q_out, T, hq, D, dt, "q_out")
-    r = mp_kv_rows(T, hq, 0 if freqs is None else 2 * freqs.numel(), MP_ROPE_INTERLEAVED if interleaved else 0,
-                   amplitude, ldk, ldv, ldq, ldqo)
+        shape = (T, hq, heads[1])
+        ldq = ldqo = _head_rows(q, shape, dt, "q")
+        if q_out is None:
+            q_out = q
+        else:
+            ldqo = _head_rows(q_out, shape, dt, "q_out")
+    r = mp_kv_rows(T, hq, rot, MP_ROPE_INTERLEAVED if interleaved else 0, amplitude, ldk, ldv, ldq, ldqo)
     _check(lib.mp_kv_append(cache._ref, C.byref(r), k.data_ptr(), v.data_ptr(), slots.data_ptr(),
-                            _ptr(positions) if freqs is not None else None, _ptr(freqs), _ptr(q),
-                            _ptr(q_out) if q is not None else None, _stream(stream)))
+                            positions.data_ptr() if rot else None, _ptr(freqs), _ptr(q), _ptr(q_out),
+                            _stream(stream)))
 
 
 def mp_kv_attend(cache: KvCache, q, table, lens, out, scale: Optional[float] = None, window: int = 0, lse=None,
@@ -747,21 +763,24 @@ def mp_kv_attend(cache: KvCache, q, table, lens, out, scale: Optional[float] = N
     ``lse``: fp32 [rows, q_heads], receives the log of the summed exponentials; ``workspace``: a device tensor of
     ``mp_kv_attend_workspace`` bytes to reuse between calls (default: a new one)."""
     import torch
-    dt, D = cache.k.dtype, cache.k.shape[3]
+    dt, D = cache._dtype, cache._shape[3]
     R, H = q.shape[:2]
-    ldq, ldo = _head_rows(q, R, H, D, dt, "q"), _head_rows(out, R, H, D, dt, "out")
-    if table.dim() != 2 or table.shape[0] != R or table.dtype is not torch.int32:
-        raise ValueError(f"table: shape {tuple(table.shape)} {table.dtype}, expected int32 of {R} rows")
-    W = table.shape[1]
+    shape = (R, H, D)
+    ldq, ldo = _head_rows(q, shape, dt, "q"), _head_rows(out, shape, dt, "out")
+    wide = table.shape
+    if len(wide) != 2 or wide[0] != R or table.dtype is not torch.int32:
+        raise ValueError(f"table: shape {tuple(wide)} {table.dtype}, expected int32 of {R} rows")
+    W = wide[1]
     st, sc = table.stride()
     if W > 1 and sc != 1:
         raise ValueError("table: the pages of a row must be adjacent")
     if R > 1 and st != 0 and st < W:
         raise ValueError(f"table: rows overlap or run backwards (stride {st})")
     _vector(lens, R, torch.int32, "lens")
-    if lse is not None and lse.shape != (R, H):
-        raise ValueError(f"lse: shape {tuple(lse.shape)}, expected {(R, H)}")
-    _vector(lse, R * H, torch.float32, "lse")
+    if lse is not None:
+        if lse.shape != (R, H):
+            raise ValueError(f"lse: shape {tuple(lse.shape)}, expected {(R, H)}")
+        _vector(lse, R * H, torch.float32, "lse")
     s = mp_kv_attend_shape(R, H, W, ldq, ldo, st if R > 1 else max(st, W), int(window),
                            D ** -0.5 if scale is None else scale)
     wp, wb, hold = _scratch(_kv_need(cache, s), workspace, q, stream)
