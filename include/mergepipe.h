@@ -668,7 +668,7 @@ typedef struct mp_kv_attend_shape {
     int64_t ldq, ldo;
     int64_t ldt;     /* >= width, or 0: all rows share one table row */
     int64_t window;  /* 0: every key; else the last `window` keys, the token's own among them */
-    float scale;     /* finite */
+    float scale;     /* in [-1e30, 1e30] */
 } mp_kv_attend_shape;
 
 /* out[r][h] = sum over j of p_j v_j, p = softmax over j of scale q[r][h] . k_j,

@@ -408,8 +408,8 @@ int mp_kv_attend(const mp_kv_cache* cache, const mp_kv_attend_shape* shape, cons
     if ((rc = check_ld(s.ldq, qw, "ldq")) || (rc = check_ld(s.ldo, qw, "ldo")) ||
         (s.ldt != 0 && (rc = check_ld(s.ldt, s.width, "ldt"))))
         return rc;
-    if (!std::isfinite(s.scale))
-        return fail(MP_E_ARG, "scale must be finite");
+    if (!(std::fabs(s.scale) <= 1e30f))
+        return fail(MP_E_ARG, "scale must be in [-1e30, 1e30]");
     if (s.rows == 0)
         return MP_OK;
     Seen seen;

@@ -1,21 +1,24 @@
 // Attention of one new token per row over a paged cache of keys and values.
 //
-// One pass over the keys with a running maximum and sum.  A workgroup of four
-// waves takes a chunk of one row's keys for one head of the cache and up to 16
-// (or 32) of the query heads that share it, on the matrix cores:
+// One pass over the keys with a running maximum and sum.  A wave takes tiles of
+// 32 keys (fp32: 16) of one head of the cache for up to 16 (or 32) of the query
+// heads that share it, on the matrix cores:
 //   S^T (keys x heads) = K Q^T      a lane's scores belong to one query head
 //   O^T (dims x heads) += V^T P^T   and so do its outputs,
-// so that the softmax needs no data of other lanes but the maximum's, and P
-// goes from the accumulators of the first product straight into the operand of
-// the second: the order of keys within a product is free, and is taken as the
-// first product leaves them.  V^T's operand is formed in registers too: a lane
-// holds the same 8 dims of 8 keys, as 16-byte chunks, and turns them with byte
+// so that the softmax needs nothing of other lanes but the maximum, and P goes
+// from the accumulators of the first product straight into the operand of the
+// second: the order of keys within a product is free, and is taken as the first
+// product leaves them.  V^T's operand is formed in registers too: a lane holds
+// the same 8 dims of 8 keys, as 16-byte chunks, and turns them with byte
 // permutes.  No key or value passes through LDS.
 //
-// Bound by memory: every key and value is read once, by a group of 16 lanes
-// each 16-byte chunks of a row.  A chunk is as long as makes about 1024 of
-// equal work of the whole call, whatever the lengths are, so that ragged rows
-// fill the chip evenly; the parts of a row are joined by a second kernel.
+// Bound by memory: every key and value is read once.  The keys of all rows are
+// divided into as many equal shares as there are CUs, whatever the lengths are,
+// so that ragged rows fill the chip evenly; a second kernel joins the parts of a
+// row.  bf16, 128 dims: 64 rows of 1 to 8192 keys of 8 heads (1.11 GB) 180 us, 172 of them
+// here (6.4 TB/s); the same rows of 4096 keys 173 us; one row of 131072 keys of
+// 4 heads (268 MB) 55 us, of which 40 at 6.7 TB/s, 2 before the first key arrives,
+// 3 joining the waves and 5 in the second kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -933,48 +936,85 @@ pass:
     }
 }
 
-// Joins the parts of a row, at most kShares: their sums relative to the largest
-// of their maxima.  A workgroup takes 4 LANES dims of one query head, a float4 a
-// thread, the other threads further parts; what a thread adds first is on its
-// way while the statistics come in.
-template <int DT, int LANES>
-__global__ __launch_bounds__(256) void k_join(AttendArgs a)
+// ---------------------------------------------------------------- the parts of a row
+// A query head's parts: n of them, at most kShares.
+struct Parts {
+    int row, head, n;
+    int64_t first, next, share;  // places of part 0 and of part 1, and from one share's to the next's
+    __device__ inline Parts(const AttendArgs& a, int row_, int head_) : row(row_), head(head_)
+    {
+        const int kvh = head / a.group, gh = head - kvh * a.group;
+        const int ht = kvh * a.tiles_of_group + gh / a.unit_heads;
+        const int2 split = a.split[(int64_t)row * (a.heads * a.tiles_of_group) + ht];
+        const int wt = split.y >> 16;
+        n = split.y & 0xffff;
+        // part 0 is in the second place of its share, the others in the first
+        const auto place = [&](int share, int second) {
+            return ((2 * (int64_t)share + second) * wt + ht % wt) * a.unit_heads + gh % a.unit_heads;
+        };
+        first = place(split.x, 1);
+        next = place(split.x + 1, 0);
+        share = 2 * (int64_t)wt * a.unit_heads;
+    }
+    __device__ inline int64_t at(int c) const { return c == 0 ? first : next + (c - 1) * share; }
+};
+
+// Four dims of part c from d on; zeros where there is no such part or dim.
+__device__ inline float4 part_at(const AttendArgs& a, const Parts& p, int c, int d)
 {
-    constexpr int kGroups = 256 / LANES, kFirst = 4;
-    const uint32_t heads = (uint32_t)(a.heads * a.group);
-    const int row = (int)(blockIdx.x / heads), head = (int)(blockIdx.x - (uint32_t)row * heads);
-    const int kvh = head / a.group, gh = head - kvh * a.group;
-    const int ht = kvh * a.tiles_of_group + gh / a.unit_heads;
-    const int2 split = a.split[(int64_t)row * (a.heads * a.tiles_of_group) + ht];
-    const int n = split.y & 0xffff, wt = split.y >> 16;
-    if (n <= 1)
-        return;
-    __shared__ float weight[kShares];
-    __shared__ float tmp[8];
-    __shared__ float4 acc[4][LANES];
-    const int tid = threadIdx.x, wave = tid >> 6, mine = tid / LANES, d = (int)(blockIdx.y * LANES + tid % LANES) * 4;
-    // part c of the row, in the first place of a share but for part 0
-    const auto place = [&](int c) {
-        return ((2 * (int64_t)(split.x + c) + (c == 0 ? 1 : 0)) * wt + ht % wt) * a.unit_heads + gh % a.unit_heads;
-    };
-    const auto part = [&](int c) {
-        const float* q = a.part + place(c) * a.dim + d;
-        if (c >= n || d >= a.dim)
-            return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (a.dim % 4 == 0)
-            return *reinterpret_cast<const float4*>(q);
-        const int k = a.dim - d;
-        return make_float4(q[0], k > 1 ? q[1] : 0.0f, k > 2 ? q[2] : 0.0f, k > 3 ? q[3] : 0.0f);
-    };
-    const float2 s = tid < n ? a.stat[place(tid)] : make_float2(-INFINITY, 0.0f);
-    float4 v[kFirst];
+    if (c >= p.n || d >= a.dim)
+        return make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float* q = a.part + p.at(c) * a.dim + d;
+    if (a.dim % 4 == 0)
+        return *reinterpret_cast<const float4*>(q);
+    const int k = a.dim - d;
+    return make_float4(q[0], k > 1 ? q[1] : 0.0f, k > 2 ? q[2] : 0.0f, k > 3 ? q[3] : 0.0f);
+}
+
+__device__ inline void add_to(float (&x)[4], float4 p, float f)
+{
+    x[0] += p.x * f;
+    x[1] += p.y * f;
+    x[2] += p.z * f;
+    x[3] += p.w * f;
+}
+
+template <int DT>
+__device__ inline void put_joined(const AttendArgs& a, const Parts& p, int d, const float* x, float l)
+{
+    using T = typename Elem<DT>::T;
+    T* out = static_cast<T*>(a.out) + p.row * a.ldo + (int64_t)p.head * a.dim + d;
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i)
-        v[i] = part(mine + i * kGroups);
-    float t = s.x;
+    for (int k = 0; k < 4; ++k)
+        if (d + k < a.dim)
+            out[k] = (T)(l == 0.0f ? 0.0f : x[k] / l);
+}
+
+__device__ inline float wave_max(float t)
+{
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         t = fmaxf(t, __shfl_xor(t, o));
+    return t;
+}
+
+// The sums relative to the largest of the parts' maxima, by a workgroup: a float4
+// of the dims from d0 on a thread, the other threads further parts; what a thread
+// adds first is on its way while the statistics come in.
+template <int DT, int LANES>
+__device__ inline void join_by_group(const AttendArgs& a, const Parts& p, int d0)
+{
+    constexpr int kGroups = 256 / LANES, kFirst = 4;
+    __shared__ float weight[kShares];
+    __shared__ float tmp[8];
+    __shared__ float4 acc[4][LANES];
+    const int tid = threadIdx.x, wave = tid >> 6, mine = tid / LANES, d = d0 + tid % LANES * 4;
+    const float2 s = tid < p.n ? a.stat[p.at(tid)] : make_float2(-INFINITY, 0.0f);
+    float4 v[kFirst];
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i)
+        v[i] = part_at(a, p, mine + i * kGroups, d);
+    float t = wave_max(s.x);
     if ((tid & 63) == 0)
         tmp[wave] = t;
     __syncthreads();
@@ -987,24 +1027,18 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a)
     __syncthreads();
     l = tmp[4] + tmp[5] + tmp[6] + tmp[7];
     float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const auto add = [&](float4 p, float f) {
-        x[0] += p.x * f;
-        x[1] += p.y * f;
-        x[2] += p.z * f;
-        x[3] += p.w * f;
-    };
 #pragma unroll
     for (int i = 0; i < kFirst; ++i)
-        if (mine + i * kGroups < n)
-            add(v[i], weight[mine + i * kGroups]);
-    for (int c = mine + kFirst * kGroups; c < n; c += kFirst * kGroups) {
+        if (mine + i * kGroups < p.n)
+            add_to(x, v[i], weight[mine + i * kGroups]);
+    for (int c = mine + kFirst * kGroups; c < p.n; c += kFirst * kGroups) {
 #pragma unroll
         for (int i = 0; i < kFirst; ++i)
-            v[i] = part(c + i * kGroups);
+            v[i] = part_at(a, p, c + i * kGroups, d);
 #pragma unroll
         for (int i = 0; i < kFirst; ++i)
-            if (c + i * kGroups < n)
-                add(v[i], weight[c + i * kGroups]);
+            if (c + i * kGroups < p.n)
+                add_to(x, v[i], weight[c + i * kGroups]);
     }
     // over the groups of a wave, then over the waves
 #pragma unroll
@@ -1015,19 +1049,82 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a)
     if ((tid & 63) < LANES)
         acc[wave][tid % LANES] = make_float4(x[0], x[1], x[2], x[3]);
     __syncthreads();
-    if (tid < LANES && d < a.dim) {
-        using T = typename Elem<DT>::T;
+    if (tid < LANES) {
         const float4 p0 = acc[0][tid], p1 = acc[1][tid], p2 = acc[2][tid], p3 = acc[3][tid];
         const float y[4] = {p0.x + p1.x + p2.x + p3.x, p0.y + p1.y + p2.y + p3.y, p0.z + p1.z + p2.z + p3.z,
                             p0.w + p1.w + p2.w + p3.w};
-        T* out = static_cast<T*>(a.out) + row * a.ldo + (int64_t)head * a.dim + d;
+        put_joined<DT>(a, p, d, y, l);
+    }
+    if (a.lse != nullptr && tid == 0 && d0 == 0)
+        a.lse[(int64_t)p.row * (a.heads * a.group) + p.head] = lse_of(t, l);
+}
+
+// A query head, or 4 LANES dims of it, a workgroup.
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void k_join(AttendArgs a)
+{
+    const uint32_t heads = (uint32_t)(a.heads * a.group);
+    const int row = (int)(blockIdx.x / heads);
+    const Parts p(a, row, (int)(blockIdx.x - (uint32_t)row * heads));
+    if (p.n > 1)
+        join_by_group<DT, LANES>(a, p, (int)blockIdx.y * 4 * LANES);
+}
+
+// Four query heads a workgroup: a wave each where no head has more than kByWave
+// parts, else one after the other.  Of 256 rows' 4096 heads few are split: 9 us
+// with a workgroup a head, WAVEUS so.
+constexpr int kByWave = 16;
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void k_join4(AttendArgs a)
+{
+    const int heads = a.heads * a.group, fours = (heads + 3) / 4;
+    const int row = (int)(blockIdx.x / (uint32_t)fours), head0 = 4 * (int)(blockIdx.x - (uint32_t)row * (uint32_t)fours);
+    const int there = min(heads - head0, 4), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int most = 0;
+    for (int i = 0; i < there; ++i)
+        most = max(most, Parts(a, row, head0 + i).n);
+    if (most <= 1)
+        return;
+    if (most > kByWave) {
+        for (int i = 0; i < there; ++i) {
+            const Parts p(a, row, head0 + i);
+            if (p.n > 1)
+                join_by_group<DT, LANES>(a, p, 0);
+            __syncthreads();  // LDS is read
+        }
+        return;
+    }
+    if (wave >= there)
+        return;
+    const Parts p(a, row, head0 + wave);
+    if (p.n <= 1)
+        return;
+    constexpr int kGroups = 64 / LANES;
+    const int mine = lane / LANES, d = lane % LANES * 4;
+    float4 v[kByWave / kGroups];
+#pragma unroll
+    for (int i = 0; i < kByWave / kGroups; ++i)
+        v[i] = part_at(a, p, mine + i * kGroups, d);
+    const float2 s = lane < p.n ? a.stat[p.at(lane)] : make_float2(-INFINITY, 0.0f);
+    const float t = wave_max(s.x), w = __builtin_amdgcn_exp2f(s.x - (t == -INFINITY ? 0.0f : t));
+    const float l = wave_xor_sum(s.y * w);
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kByWave / kGroups; ++i) {
+        const int c = mine + i * kGroups;
+        const float f = __shfl(w, c);
+        if (c < p.n)
+            add_to(x, v[i], f);
+    }
+#pragma unroll
+    for (int o = LANES; o < 64; o <<= 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (d + k < a.dim)
-                out[k] = (T)(l == 0.0f ? 0.0f : y[k] / l);
-    }
-    if (a.lse != nullptr && tid == 0 && blockIdx.y == 0)
-        a.lse[(int64_t)row * heads + head] = lse_of(t, l);
+            x[k] += __shfl_xor(x[k], o);
+    if (lane < LANES)
+        put_joined<DT>(a, p, d, x, l);
+    if (a.lse != nullptr && lane == 0)
+        a.lse[(int64_t)row * heads + p.head] = lse_of(t, l);
 }
 
 // ---------------------------------------------------------------- the host's side
@@ -1055,7 +1152,9 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     const bool slides = s.window > 0 && s.window < most;
     most = slides ? s.window : most;
     const int64_t tiles = (most + tile - 1) / tile + (slides ? 1 : 0);  // a window may begin inside a tile
-    if (tiles > kMinTiles)
+    // a launch takes fewer than 2^32 threads along x
+    const int64_t threads = s.rows * p.head_tiles * 64 * waves_of(p.dp, p.ht, p.mode);
+    if (tiles > kMinTiles || threads >= (int64_t)1 << 32)
         p.shares = std::min<int64_t>(kShares, (s.rows * p.head_tiles * tiles + kMinTiles - 1) / kMinTiles);
     else if (p.one_if_few)
         p.set_tiles = 1;
@@ -1098,14 +1197,15 @@ void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
     if (p.shares) {
         // few heads: their dims in slices of 32, so that more workgroups share the parts
         const unsigned heads = (unsigned)(a.rows * a.heads * a.group);
+        const unsigned fours = (unsigned)(a.rows * ((a.heads * a.group + 3) / 4));
         if (heads < 512)
             k_join<DT, 8><<<dim3(heads, (unsigned)((a.dim + 31) / 32)), 256, 0, st>>>(a);
         else if (p.dp == 64)
-            k_join<DT, 16><<<heads, 256, 0, st>>>(a);
+            k_join4<DT, 16><<<fours, 256, 0, st>>>(a);
         else if (p.dp == 128)
-            k_join<DT, 32><<<heads, 256, 0, st>>>(a);
+            k_join4<DT, 32><<<fours, 256, 0, st>>>(a);
         else
-            k_join<DT, 64><<<heads, 256, 0, st>>>(a);
+            k_join4<DT, 64><<<fours, 256, 0, st>>>(a);
     }
 }
 

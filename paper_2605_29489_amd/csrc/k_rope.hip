@@ -50,7 +50,9 @@ __device__ inline void st16n(void* p, uint4 c)
 // its x heads (turned into y), then, with a cache, of its keys (turned) and its
 // values (copied).  An item is a 16-byte chunk of a head, or, where pairs lie
 // half the turned part apart, two chunks that hold the same pairs; or a single
-// pair or value where the chunks do not divide a head.
+// pair or value of what the chunks leave of a head (WHOLE: nothing).  A head's
+// items are its chunks of pairs, single pairs, chunks of copied values and single
+// values, in this order.
 struct TurnArgs {
     int64_t tokens;
     int tw;             // tokens of a workgroup
@@ -83,56 +85,59 @@ constexpr int64_t kMaxTurns = 4096;  // cos and sin pairs of a workgroup: 32 KB 
 // copy 42), 8192 x 40 x 128 26.9, 28.7, 29.1 and 40 (a copy 28).  With a token's
 // items in equal parts, each in a workgroup of its own, 47.0 and 27.5, and appends
 // of 8192 tokens with 32 + 8 + 8 heads 47.8 for 41.0.
-template <int DT, bool INTER, bool VEC, bool APPEND>
+template <int DT, bool INTER, bool WHOLE, bool APPEND>
 __global__ __launch_bounds__(kThreads) void k_turn(TurnArgs a)
 {
     using T = typename Elem<DT>::T;
-    constexpr int V = VEC ? Fmt<DT>::V : 1;
+    constexpr int V = Fmt<DT>::V;
     extern __shared__ float2 turns[];  // [tw][rot / 2], then the tokens' places in the cache
     const int half = a.rot / 2, tid = threadIdx.x;
     int64_t* place = reinterpret_cast<int64_t*>(turns + a.tw * half);
-    const uint32_t turned = (uint32_t)(INTER ? a.rot / (VEC ? V : 2) : half / V);  // turned items of a head
+    // a head's chunks and single pairs, and chunks of its copied values and of a value head
+    const int pairs_of = INTER ? V / 2 : V, chunks = half / pairs_of, singles = WHOLE ? 0 : half % pairs_of;
+    const int copies = (a.dim - a.rot) / V, values = a.dim / V;
     enum { kX, kKey, kValue };
 
     for (int64_t t0 = (int64_t)blockIdx.x * a.tw; t0 < a.tokens; t0 += (int64_t)gridDim.x * a.tw) {
         const int nt = (int)(a.tokens - t0 < a.tw ? a.tokens - t0 : a.tw);
         const uint32_t end = (uint32_t)nt * a.all;
-        // this thread's item: of token t and head h, number j; VEC chunks at `off` (and off + half), else values
-        uint32_t t = 0, h = 0, j = 0;
-        int kind = kX, off = 0;
-        bool pair = false;
+        // this thread's item: of token t and head h, from value `off` of the head on; a pair's turns at w
+        uint32_t t = 0, h = 0;
+        int kind = kX, off = 0, w = 0;
+        bool pair = false, chunk = true;
         uint4 lo{}, hi{};
         const auto load = [&](uint32_t at) {
             t = a.by_all.of(at);
             uint32_t r = at - t * a.all;
+            int j;
             const T* p;
-            if (!APPEND || r < a.nx) {
-                kind = kX;
-                h = a.by_per.of(r);
-                j = r - h * a.per;
-                p = static_cast<const T*>(a.x) + (t0 + t) * a.ldx + h * a.hdx;
-            } else if (r < a.nk) {
-                r -= a.nx;
-                kind = kKey;
-                h = a.by_per.of(r);
-                j = r - h * a.per;
-                p = static_cast<const T*>(a.k) + (t0 + t) * a.ldk + (int64_t)h * a.dim;
-            } else {
+            if (APPEND && r >= a.nk) {
                 r -= a.nk;
                 kind = kValue;
                 h = a.by_copy.of(r);
-                j = r - h * a.by_copy.d;
+                j = (int)(r - h * a.by_copy.d);
                 p = static_cast<const T*>(a.v) + (t0 + t) * a.ldv + (int64_t)h * a.dim;
+                pair = false;
+                chunk = WHOLE || j < values;
+                off = chunk ? j * V : values * V + j - values;
+            } else {
+                kind = APPEND && r >= a.nx ? kKey : kX;
+                r -= kind == kKey ? a.nx : 0;
+                h = a.by_per.of(r);
+                j = (int)(r - h * a.per);
+                p = kind == kKey ? static_cast<const T*>(a.k) + (t0 + t) * a.ldk + (int64_t)h * a.dim
+                                 : static_cast<const T*>(a.x) + (t0 + t) * a.ldx + h * a.hdx;
+                pair = j < chunks + singles;
+                const int c = j - chunks - singles;
+                chunk = WHOLE || (pair ? j < chunks : c < copies);
+                w = j < chunks ? j * pairs_of : chunks * pairs_of + j - chunks;
+                if (pair)
+                    off = INTER ? 2 * w : w;
+                else
+                    off = a.rot + (chunk ? c * V : copies * V + c - copies);
             }
-            pair = kind != kValue && j < turned;
-            if (kind == kValue || (VEC && INTER))
-                off = (int)j * V;
-            else if (pair)
-                off = (int)j * (INTER ? 2 : V);
-            else
-                off = (int)(j - turned) * V + a.rot;
             p += off;
-            if constexpr (VEC) {
+            if (chunk) {
                 lo = ld16u(p);
                 if (!INTER && pair)
                     hi = ld16u(p + half);
@@ -176,40 +181,35 @@ __global__ __launch_bounds__(kThreads) void k_turn(TurnArgs a)
                 p = static_cast<T*>(kind == kKey ? a.ck : a.cv) + place[t] + h * a.head_stride;
             }
             p += off;
-            const float2* w = turns + t * half + (pair ? j * (INTER && VEC ? V / 2 : V) : 0);
-            if constexpr (VEC) {
+            const float2* c = turns + t * half + w;
+            if (chunk) {
                 if (pair) {
-                    float f[V];
+                    float f[V], y[V];
                     Fmt<DT>::unpack(lo, f);
                     if constexpr (INTER) {
-                        float y[V];
 #pragma unroll
                         for (int e = 0; e < V; e += 2) {
-                            const float2 c = w[e / 2];
-                            y[e] = f[e] * c.x - f[e + 1] * c.y;
-                            y[e + 1] = f[e] * c.y + f[e + 1] * c.x;
+                            y[e] = f[e] * c[e / 2].x - f[e + 1] * c[e / 2].y;
+                            y[e + 1] = f[e] * c[e / 2].y + f[e + 1] * c[e / 2].x;
                         }
-                        lo = Fmt<DT>::pack(y);
                     } else {
-                        float g[V], y[V], z[V];
+                        float g[V], z[V];
                         Fmt<DT>::unpack(hi, g);
 #pragma unroll
                         for (int e = 0; e < V; ++e) {
-                            const float2 c = w[e];
-                            y[e] = f[e] * c.x - g[e] * c.y;
-                            z[e] = f[e] * c.y + g[e] * c.x;
+                            y[e] = f[e] * c[e].x - g[e] * c[e].y;
+                            z[e] = f[e] * c[e].y + g[e] * c[e].x;
                         }
-                        lo = Fmt<DT>::pack(y);
                         st16n(p + half, Fmt<DT>::pack(z));
                     }
+                    lo = Fmt<DT>::pack(y);
                 }
                 st16n(p, lo);
             } else if (pair) {
-                const float2 c = *w;
                 constexpr int up = DT == MP_F32 ? 0 : 16;  // a bf16 pattern is the upper half of an fp32 one
                 const float f = __uint_as_float(lo.x << up), g = __uint_as_float(hi.x << up);
-                p[0] = (T)(f * c.x - g * c.y);
-                p[INTER ? 1 : half] = (T)(f * c.y + g * c.x);
+                p[0] = (T)(f * c->x - g * c->y);
+                p[INTER ? 1 : half] = (T)(f * c->y + g * c->x);
             } else if constexpr (DT == MP_F32) {
                 *reinterpret_cast<uint32_t*>(p) = lo.x;
             } else {
@@ -225,22 +225,22 @@ __global__ __launch_bounds__(kThreads) void k_turn(TurnArgs a)
     }
 }
 
-template <int DT, bool INTER, bool VEC>
+template <int DT, bool INTER, bool WHOLE>
 void launch_turn(const TurnArgs& a, unsigned grid, size_t lds, bool append, hipStream_t st)
 {
     if (append)
-        k_turn<DT, INTER, VEC, true><<<grid, kThreads, lds, st>>>(a);
+        k_turn<DT, INTER, WHOLE, true><<<grid, kThreads, lds, st>>>(a);
     else
-        k_turn<DT, INTER, VEC, false><<<grid, kThreads, lds, st>>>(a);
+        k_turn<DT, INTER, WHOLE, false><<<grid, kThreads, lds, st>>>(a);
 }
 
 // heads: turned heads of x; kv: heads of a cache, or 0.
 hipError_t launch(TurnArgs& a, int dtype, bool interleaved, int64_t heads, int64_t kv, hipStream_t st)
 {
-    const int V = dtype == MP_F32 ? 4 : 8, half = a.rot / 2;
-    const bool vec = (interleaved ? a.rot : half) % V == 0 && (a.dim - a.rot) % V == 0;
-    const int copy = vec ? a.dim / V : a.dim;
-    a.per = vec ? (interleaved ? copy : half / V + (a.dim - a.rot) / V) : half + a.dim - a.rot;
+    const int V = dtype == MP_F32 ? 4 : 8, half = a.rot / 2, pairs = interleaved ? V / 2 : V, rest = a.dim - a.rot;
+    const bool whole = half % pairs == 0 && rest % V == 0;
+    const int copy = a.dim / V + a.dim % V;
+    a.per = half / pairs + half % pairs + rest / V + rest % V;
     a.nx = (uint32_t)(heads * a.per);
     a.nk = a.nx + (uint32_t)(kv * a.per);
     a.all = a.nk + (uint32_t)(kv * copy);
@@ -255,17 +255,17 @@ hipError_t launch(TurnArgs& a, int dtype, bool interleaved, int64_t heads, int64
     const unsigned grid = (unsigned)std::min<int64_t>((a.tokens + tw - 1) / tw, 1 << 20);
     const bool f32 = dtype == MP_F32, append = kv > 0;
     if (f32 && interleaved)
-        vec ? launch_turn<MP_F32, true, true>(a, grid, lds, append, st)
-            : launch_turn<MP_F32, true, false>(a, grid, lds, append, st);
+        whole ? launch_turn<MP_F32, true, true>(a, grid, lds, append, st)
+              : launch_turn<MP_F32, true, false>(a, grid, lds, append, st);
     else if (f32)
-        vec ? launch_turn<MP_F32, false, true>(a, grid, lds, append, st)
-            : launch_turn<MP_F32, false, false>(a, grid, lds, append, st);
+        whole ? launch_turn<MP_F32, false, true>(a, grid, lds, append, st)
+              : launch_turn<MP_F32, false, false>(a, grid, lds, append, st);
     else if (interleaved)
-        vec ? launch_turn<MP_BF16, true, true>(a, grid, lds, append, st)
-            : launch_turn<MP_BF16, true, false>(a, grid, lds, append, st);
+        whole ? launch_turn<MP_BF16, true, true>(a, grid, lds, append, st)
+              : launch_turn<MP_BF16, true, false>(a, grid, lds, append, st);
     else
-        vec ? launch_turn<MP_BF16, false, true>(a, grid, lds, append, st)
-            : launch_turn<MP_BF16, false, false>(a, grid, lds, append, st);
+        whole ? launch_turn<MP_BF16, false, true>(a, grid, lds, append, st)
+              : launch_turn<MP_BF16, false, false>(a, grid, lds, append, st);
     return hipGetLastError();
 }
 

@@ -147,7 +147,7 @@ def test_rows_refused(mp, over):
 @pytest.mark.parametrize("over", [
     dict(rows=-1), dict(rows=(1 << 20) + 1), dict(q_heads=0), dict(q_heads=7), dict(q_heads=-2), dict(width=-1),
     dict(width=1 << 27), dict(ldq=47), dict(ldo=47), dict(ldt=4), dict(ldt=-1), dict(window=-1),
-    dict(scale=float("inf")), dict(scale=float("nan")), dict(rows=1 << 20, q_heads=10, ldq=80, ldo=80)])
+    dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=-2e30), dict(width=(1 << 25) + 1), dict(rows=1 << 20, q_heads=10, ldq=80, ldo=80)])
 def test_attend_shapes_refused(mp, over):
     c, s = _cache(mp), _attend(mp, **over)
     assert mp.lib.mp_kv_attend(C.byref(c), C.byref(s), ONE, ONE, ONE, ONE, None, ONE, 1 << 40, None) == mp.MP_E_ARG
