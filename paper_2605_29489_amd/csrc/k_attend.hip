@@ -70,7 +70,7 @@ struct AttendArgs {
     int32_t rows, page_size, heads, group, dim;
     int32_t tiles_of_group;  // head tiles of the query heads that share a head of the cache
     int32_t unit_heads;      // query heads of a head tile, at most
-    int32_t set_tiles;       // head tiles of a workgroup, a head set: a power of two that divides a row's
+    int32_t set_tiles;       // head tiles of a workgroup, a head set: a power of two; a row's last set may have fewer
     int32_t one_if_few;      // or one, where the call's tiles are few
     int32_t shares;          // 0: a workgroup per row and head set
     Div by_page, by_tiles, by_heads;  // page_size, tiles_of_group, unit_heads
@@ -173,9 +173,12 @@ __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* o
     const uint32_t head_tiles = (uint32_t)(a.heads * a.tiles_of_group);
     const bool few = total * head_tiles < 2 * kShares * NW;
     out->set_tiles = a.one_if_few && few ? 1 : (uint32_t)a.set_tiles;
-    const uint32_t sets = head_tiles / out->set_tiles;
+    const uint32_t sets = (head_tiles + out->set_tiles - 1) / out->set_tiles;
     const uint64_t all = total * sets, even = quotient(all + a.shares - 1, (uint32_t)a.shares);
-    out->per = even < kMinTiles ? (uint32_t)kMinTiles : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
+    // a share holds kMinTiles at least, but no more than a row has where rows are
+    // short: 132 of 1 tile (fp32) 21.5 us in shares of 4 and 9.6 of 1
+    const uint32_t row = (uint32_t)min(quotient(total + a.rows - 1, (uint32_t)a.rows), (uint64_t)kMinTiles);
+    out->per = even < row ? row : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
     out->at = (uint64_t)number * out->per;
     out->end = min(all, out->at + out->per);
     out->row = 0;
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
     const int wt = uniform((int)share.set_tiles);
     // waves that share a head tile, and this one's head tile and place among them
     const int step = NW / wt, mine = wave / step, place = wave % step;
-    const uint32_t sets = head_tiles / (uint32_t)wt;
+    const uint32_t sets = (head_tiles + wt - 1) / (uint32_t)wt;
 
     // The tiles of one row and head set that a share takes.
     struct Run {
@@ -405,7 +408,8 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
         r.n = keys.n;
         const int tile0 = keys.lo / KT + (int)off;
         r.begin = tile0 + place;
-        r.end = keys.n <= keys.lo ? r.begin : tile0 + (int)r.n_tiles;  // a row without keys has no tiles
+        // no tiles: a row without keys, and a head tile that is not there
+        r.end = keys.n <= keys.lo || set * wt + mine >= head_tiles ? r.begin : tile0 + (int)r.n_tiles;
         return r;
     };
     // The run behind r, if `left` tiles of the share lie behind it.
@@ -608,7 +612,7 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
 
     for (;;) {
         const bool whole = cur.n_tiles == cur.work;
-        if (cur.off == 0 && tid < wt && a.split != nullptr)
+        if (cur.off == 0 && tid < wt && cur.set * wt + tid < head_tiles && a.split != nullptr)
             a.split[(int64_t)cur.row * head_tiles + cur.set * wt + tid] =
                 make_int2((int)blockIdx.x, (whole ? 1 : parts ? parts : (int)((before + cur.work - 1) / per) + 1) | wt << 16);
 
@@ -771,7 +775,8 @@ pass:
         }
         for (; barriers > 0; --barriers)
             __builtin_amdgcn_s_barrier();
-        const Heads hd = heads_of(cur.set * wt + mine);
+        const bool there = cur.set * wt + mine < head_tiles;
+        const Heads hd = heads_of(there ? cur.set * wt + mine : 0);
         if constexpr (kBf16)
             if (!again) {
                 bool nan = false;
@@ -801,7 +806,7 @@ pass:
 #pragma unroll
             for (int h = 0; h < HT; ++h) {
                 const int head = 16 * h + m;
-                if (head >= hd.nh)
+                if (head >= hd.nh || !there)
                     continue;
                 const float r = sum[h] == 0.0f ? 0.0f : whole ? 1.0f / sum[h] : 1.0f;
                 T* out = static_cast<T*>(a.out) + cur.row * a.ldo + (head0 + head) * a.dim;
@@ -890,6 +895,8 @@ pass:
             constexpr int D4 = DP / 4;
             for (int i = tid / D4, d = tid % D4 * 4; i < wt * a.unit_heads; i += 64 * NW / D4) {
                 const int t = (int)a.by_heads.of((uint32_t)i), h = i - t * a.unit_heads;
+                if (cur.set * wt + t >= head_tiles)
+                    break;
                 const Heads of = heads_of(cur.set * wt + t);
                 if (h >= of.nh || d >= a.dim)
                     continue;
@@ -1071,8 +1078,8 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a)
 }
 
 // Four query heads a workgroup: a wave each where no head has more than kByWave
-// parts, else one after the other.  Of 256 rows' 4096 heads few are split: 9 us
-// with a workgroup a head, WAVEUS so.
+// parts, else one after the other.  256 rows of 16 heads, few of them split: 8.9
+// us with a workgroup a head, 6.5 so.
 constexpr int kByWave = 16;
 template <int DT, int LANES>
 __global__ __launch_bounds__(256) void k_join4(AttendArgs a)
@@ -1145,8 +1152,11 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     p.ht = group > 16 && dim <= 128 ? 2 : 1;
     p.head_tiles = c.heads * ((group + 16 * p.ht - 1) / (16 * p.ht));
     p.unit_heads = std::min<int64_t>(group, 16 * p.ht);
-    while (p.set_tiles < waves_of(p.dp, p.ht, p.mode) && p.head_tiles % (2 * p.set_tiles) == 0)
-        p.set_tiles *= 2;
+    // the largest set that leaves no more than a quarter of the waves idle in a row's sets
+    const auto waste = [&](int64_t n) { return (p.head_tiles + n - 1) / n * n - p.head_tiles; };
+    p.set_tiles = waves_of(p.dp, p.ht, p.mode);
+    while (4 * waste(p.set_tiles) > p.head_tiles + waste(p.set_tiles))
+        p.set_tiles /= 2;
     p.one_if_few = s.rows * p.head_tiles < kShares;
     int64_t most = s.width * c.page_size;
     const bool slides = s.window > 0 && s.window < most;
@@ -1187,7 +1197,7 @@ void launch_tiles(const AttendArgs& a, unsigned grid, int mode, hipStream_t st)
 template <int DT>
 void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
 {
-    const unsigned grid = (unsigned)(p.shares ? p.shares : a.rows * (p.head_tiles / p.set_tiles));
+    const unsigned grid = (unsigned)(p.shares ? p.shares : a.rows * ((p.head_tiles + p.set_tiles - 1) / p.set_tiles));
     if (p.dp == 64)
         p.ht == 2 ? launch_tiles<DT, 64, 2>(a, grid, p.mode, st) : launch_tiles<DT, 64, 1>(a, grid, p.mode, st);
     else if (p.dp == 128)

@@ -118,6 +118,10 @@ ROPE = [  # tokens, heads, dim, rot, interleaved, pad, tokens inside, first posi
     (6, 2, 4096, 4096, True, 0, False, 7, 1.0),
     (2, 70, 24, 24, False, 0, False, 2 ** 31 + 7, 1.0),
     (4, 1, 128, 128, False, 9, False, 2 ** 40, 1.0),
+    (40, 3, 134, 110, False, 1, False, 77, 1.0),
+    (40, 3, 140, 134, True, 0, True, 77, 1.0),
+    (2000, 1, 6, 4, False, 0, False, 0, 1.0),
+    (5, 300, 64, 64, False, 0, False, 9, 1.0),
 ]
 
 
@@ -367,6 +371,16 @@ ATTEND = [  # lengths, heads, group, dim, page, layout, window
     ([1700, 600, 599], 2, 3, 72, 10, "tokens", 600),
     ([40], 1, 1, 128, 16, "tokens", 2 ** 40),
     ([90] * 300, 1, 2, 64, 16, "tokens", 0),
+    ([40, 3, 200, 1, 0, 17] * 200, 1, 1, 64, 16, "tokens", 0),     # more rows than threads
+    ([40, 3, 0, 1, 150] * 130, 1, 3, 128, 16, "heads", 0),
+    ([9, 130] * 300, 1, 2, 72, 10, "tokens", 0),
+    ([300, 2, 90, 0] * 20, 16, 1, 64, 32, "tokens", 0),            # a head a wave
+    ([260, 31, 700, 5] * 10, 8, 2, 128, 16, "tokens", 0),
+    ([5, 140, 33], 15, 2, 128, 16, "heads", 0),                    # sets with a wave to spare
+    ([5, 340, 33, 90], 13, 3, 96, 16, "tokens", 50),
+    ([5, 140, 33], 3, 20, 256, 16, "heads", 0),
+    ([3, 1], 31, 38, 256, 16, "tokens", 0),
+    ([4000] + [1] * 40, 8, 1, 64, 16, "heads", 0),                 # one long row among short ones
     ([1500, 20] + [3] * 290, 2, 2, 64, 16, "heads", 0),
 ]
 
@@ -431,6 +445,85 @@ def test_attend_pages_outside_the_cache_and_lengths_out_of_range(mp, dtype, page
         _near(out[i], w[0].reshape(H, dim), w[2].reshape(H, dim), f"out {i}")
         _near(lse[i], w[1].reshape(H), w[3].reshape(H), f"lse {i}")
     assert (out[[1, 5]] == 0).all() and torch.isneginf(lse[[1, 5]]).all()
+
+
+@pytest.mark.parametrize("heads,dim,rows,n", [(16, 64, 20, 500), (8, 128, 40, 300), (2, 128, 1, 9000),
+                                              (3, 256, 3, 800)])
+def test_attend_infinite_values_among_exact_ones(mp, heads, dim, rows, n):
+    """An infinite value reaches its own dim of the heads that read it, and changes nothing else by a bit."""
+    import torch
+    rng = np.random.default_rng(heads)
+    page, group = 16, 2
+    table, pages = _paged(rng, [n] * rows, page)
+    c = _new_cache(mp, "bf16", pages, page, heads, dim, "tokens")
+    _fill(rng, c, table, [n] * rows, page)
+    q = _dev(rng.standard_normal((rows, heads * group, dim)), "bf16")
+    T, L = torch.from_numpy(table).cuda(), torch.full((rows,), n, dtype=torch.int32, device="cuda")
+    want = torch.empty_like(q)
+    mp.mp_kv_attend(c, q, T, L, want)
+    for row, j, h, d, x in ((0, 0, 0, 3, "inf"), (rows - 1, n - 1, heads - 1, dim - 1, "-inf"),
+                            (rows // 2, n // 2, 1, 9, "nan")):
+        c.v[int(table[row, j // page]), j % page, h, d] = float(x)
+        want[row, h * group:(h + 1) * group, d] = float(x)
+    out = torch.empty_like(q)
+    mp.mp_kv_attend(c, q, T, L, out)
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(out), nan)
+    assert torch.equal(out[~nan], want[~nan])
+
+
+def test_attend_many_rows_of_one_sequence(mp):
+    """A million rows share a table row: more workgroups than a launch holds threads for."""
+    import torch
+    rng = np.random.default_rng(4)
+    rows, heads, dim, page = 1 << 20, 7, 64, 16
+    c = _new_cache(mp, "bf16", 9, page, heads, dim, "tokens", rng)
+    K, V = (_host(t).reshape(-1, heads, dim) for t in (c.k, c.v))
+    table = np.array([[3, 8]], np.int32)
+    q = torch.randn(rows, heads, dim, dtype=torch.bfloat16, device="cuda")
+    lens = (torch.arange(rows, device="cuda") % 33).int()
+    out, lse = torch.full_like(q, float("nan")), torch.full((rows, heads), float("nan"), device="cuda")
+    mp.mp_kv_attend(c, q, torch.from_numpy(table).cuda().expand(rows, -1), lens, out, lse=lse)
+    torch.cuda.synchronize()
+    for i in [0, 1, 32, 33, 4095, 4096, 65537, rows // 2 + 5, rows - 2, rows - 1]:
+        n = i % 33
+        w = _attention(_host(q[i])[:, None], K, V, _slots(table[0], n, page, 0, 9), dim ** -0.5, "bf16")
+        _near(out[i], w[0][:, 0], w[2][:, 0], f"out {i}")
+        _near(lse[i], w[1][:, 0], w[3][:, 0], f"lse {i}")
+    assert not torch.isnan(out).any() and torch.equal(torch.isneginf(lse).all(1), lens == 0)
+
+
+def test_attend_splits_do_not_change_what_a_row_is(mp):
+    """A row alone, among others and cut in two that lse joins: within the tolerance of each other."""
+    import torch
+    rng = np.random.default_rng(12)
+    page, heads, group, dim, n = 16, 2, 3, 128, 5000
+    table, pages = _paged(rng, [n, 40, 900], page)
+    c = _new_cache(mp, "f32", pages, page, heads, dim, "tokens")
+    K, V = _fill(rng, c, table, [n, 40, 900], page)
+    q = _dev(rng.standard_normal((3, heads * group, dim)), "f32")
+    T = torch.from_numpy(table).cuda()
+
+    def attend(rows, table, lens):
+        out, lse = torch.empty(len(rows), heads * group, dim, device="cuda"), torch.empty(len(rows), 6, device="cuda")
+        mp.mp_kv_attend(c, q[rows], table, torch.tensor(lens, dtype=torch.int32, device="cuda"), out, lse=lse)
+        return out, lse
+    together, alone = attend([0, 1, 2], T, [n, 40, 900]), attend([0], T[:1], [n])
+    cut = 2000
+    a = attend([0], T[:1, :cut // page].contiguous(), [cut])
+    b = attend([0], T[:1, cut // page:].contiguous(), [n - cut])
+    la, lb = _host(a[1])[..., None], _host(b[1])[..., None]
+    lse = np.logaddexp(la, lb)
+    joined = np.exp(la - lse) * _host(a[0]) + np.exp(lb - lse) * _host(b[0])
+    slots = _slots(table[0], n, page, 0, pages)
+    w = _attention(_host(q[0]).reshape(heads, group, dim), K, V, slots, dim ** -0.5, "f32")
+    want, tol = w[0].reshape(1, 6, dim), w[2].reshape(1, 6, dim)
+    _near(together[0][:1], want, tol, "together")
+    _near(alone[0], want, tol, "alone")
+    # a part is off by no more than the whole may be, having fewer keys, and the parts' weights sum to 1; the error of
+    # either lse moves those weights by that much of sum p |v| again
+    assert (np.abs(joined - want) <= 3 * tol).all()
+    assert (np.abs(lse[..., 0] - w[1].reshape(1, 6)) <= 3 * w[3].reshape(1, 6)).all()
 
 
 def test_attend_empty_tables_and_caches(mp):
