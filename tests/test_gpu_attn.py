@@ -792,3 +792,14 @@ class _Null:
 
     def data_ptr(self):
         return 0
+
+
+def test_example_serves_a_merge(mp):
+    """The example runs, its graph replays the eager step's bits, and its rotary gradient is the transpose."""
+    import torch
+    from examples import decode
+    y, same, apart, dots, scale = decode.main(prompt=40, steps=4, say=lambda s: None)
+    assert same and torch.isfinite(y).all()
+    # each of the two sums of products of bf16 values carries the roundings of its turned factor, 2^-8 at most, and of
+    # the turn itself; a pair's products are at most twice those of the untouched values
+    assert abs(dots[0] - dots[1]) <= 2 * 2 * (2.0 ** -8 + 2 * TURN) * 2 * scale
