@@ -77,15 +77,20 @@ struct AttendArgs {
     float scale;  // times log2(e)
 };
 
-// A lane's keys of a row: [lo, n).
+// A length or a page, which no kernel here writes: where the address is one for
+// the wave it comes through the scalar cache.
+__device__ inline int32_t ld_constant(const int32_t* p)
+{
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// The keys of a row: [lo, n).
 struct Range {
     int32_t lo, n;
 };
 __device__ inline Range range_of(const AttendArgs& a, int row)
 {
-    // the kernel writes no length: read so, a wave's own row comes through the scalar cache
-    const int32_t len = *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
-        reinterpret_cast<uintptr_t>(a.lens + row));
+    const int32_t len = ld_constant(a.lens + row);
     const int32_t n = len < 0 ? 0 : len < a.most ? len : a.most;
     return {n > a.window ? n - (int32_t)a.window : 0, n};
 }
@@ -491,7 +496,9 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
             return c;
         constexpr int bits = 8 * es;
         const int drop = (4 * V * s + V * g - chunk_at(s)) * bits;
-        const auto keep = [&](int w) { return drop <= 32 * w ? ~0u : drop >= 32 * w + 32 ? 0u : ~0u << (drop - 32 * w); };
+        const auto keep = [&](int w) {
+            return drop <= 32 * w ? ~0u : drop >= 32 * w + 32 ? 0u : ~0u << (drop - 32 * w);
+        };
         return make_uint4(c.x & keep(0), c.y & keep(1), c.z & keep(2), c.w & keep(3));
     };
     const auto value_at = [&](int c, int mm) {
@@ -503,8 +510,8 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
 #pragma unroll
         for (int h = 0; h < HT; ++h) {
             // heads that are not there take the last one's place: their results are not used
-            const char* qp = static_cast<const char*>(a.q) +
-                             (r.row * a.ldq + (int64_t)(hd.kvh * a.group + hd.gh0 + min(16 * h + m, hd.nh - 1)) * a.dim) * es;
+            const int64_t head = hd.kvh * a.group + hd.gh0 + min(16 * h + m, hd.nh - 1);
+            const char* qp = static_cast<const char*>(a.q) + (r.row * a.ldq + head * a.dim) * es;
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 q[h][s] = MODE == kOdd ? ld16_few<DT>(qp, 4 * V * s + V * g, a.dim) : ld16u(qp + chunk_at(s) * es);
@@ -518,8 +525,7 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
         if constexpr (kUni) {
 #pragma unroll
             for (int j = 0; j < KG; ++j)
-                page[j] = *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(
-                    table + a.by_page.of((uint32_t)min(c.tile * KT + 16 * j, c.run.n - 1))));
+                page[j] = ld_constant(table + a.by_page.of((uint32_t)min(c.tile * KT + 16 * j, c.run.n - 1)));
         } else {
             page[0] = table[a.by_page.of((uint32_t)min(c.tile * KT + lane % KT, c.run.n - 1))];
         }
@@ -556,7 +562,10 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
                 const char* row = a.k + max((int64_t)__shfl(where[0], 16 * j + m), (int64_t)0);
 #pragma unroll
                 for (int s = 0; s < S; ++s)
-                    kr[j][s] = MODE == kOdd ? ld16_few<DT>(row, 4 * V * s + V * g, a.dim) : ld16u(row + chunk_at(s) * es);
+                    if constexpr (MODE == kOdd)
+                        kr[j][s] = ld16_few<DT>(row, 4 * V * s + V * g, a.dim);
+                    else
+                        kr[j][s] = ld16u(row + chunk_at(s) * es);
             }
         }
     };
@@ -587,7 +596,7 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
 #pragma unroll
                     for (int c = 0; c < NC; ++c)
                         if constexpr (MODE == kOdd)
-                            vr[4 * j + e][c] = ld16_few<DT>(row, 16 * W * c + W * m, min(a.dim, 16 * W * c + W * m + W));
+                            vr[4 * j + e][c] = ld16_few<DT>(row, value_at(c, m), min(a.dim, value_at(c, m) + W));
                         else
                             vr[4 * j + e][c] = ld_values<WB>(row + value_at(c, m) * es);
                 }
@@ -612,9 +621,10 @@ __global__ __launch_bounds__(64 * waves_of(DP, HT, MODE)) void k_attend(AttendAr
 
     for (;;) {
         const bool whole = cur.n_tiles == cur.work;
-        if (cur.off == 0 && tid < wt && cur.set * wt + tid < head_tiles && a.split != nullptr)
-            a.split[(int64_t)cur.row * head_tiles + cur.set * wt + tid] =
-                make_int2((int)blockIdx.x, (whole ? 1 : parts ? parts : (int)((before + cur.work - 1) / per) + 1) | wt << 16);
+        if (cur.off == 0 && tid < wt && cur.set * wt + tid < head_tiles && a.split != nullptr) {
+            const int n = whole ? 1 : parts ? parts : (int)((before + cur.work - 1) / per) + 1;
+            a.split[(int64_t)cur.row * head_tiles + cur.set * wt + tid] = make_int2((int)blockIdx.x, n | wt << 16);
+        }
 
         f32x4 o[HT][NC * W];
         float top[HT], sum[HT];
@@ -1085,7 +1095,8 @@ template <int DT, int LANES>
 __global__ __launch_bounds__(256) void k_join4(AttendArgs a)
 {
     const int heads = a.heads * a.group, fours = (heads + 3) / 4;
-    const int row = (int)(blockIdx.x / (uint32_t)fours), head0 = 4 * (int)(blockIdx.x - (uint32_t)row * (uint32_t)fours);
+    const int row = (int)(blockIdx.x / (uint32_t)fours);
+    const int head0 = 4 * (int)(blockIdx.x - (uint32_t)row * (uint32_t)fours);
     const int there = min(heads - head0, 4), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int most = 0;
     for (int i = 0; i < there; ++i)
@@ -1149,10 +1160,14 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     const int64_t group = s.q_heads / c.heads, tile = c.dtype == MP_F32 ? 16 : 32;
     p.dp = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
     p.mode = dim < V ? kOdd : c.page_size % 16 != 0 ? kEven : dim == p.dp ? kWhole : kRows;
+    // Groups of more than 16 heads read their keys once for 32, with half the waves: 32 rows of up to 8192 keys, 8
+    // heads for 32 each, 128 dims, 117 us; 16 at a time 144.  256 dims leave no registers for it.
     p.ht = group > 16 && dim <= 128 ? 2 : 1;
     p.head_tiles = c.heads * ((group + 16 * p.ht - 1) / (16 * p.ht));
     p.unit_heads = std::min<int64_t>(group, 16 * p.ht);
-    // the largest set that leaves no more than a quarter of the waves idle in a row's sets
+    // The largest set that leaves no more than a quarter of the waves idle in a row's sets: the heads of a token are
+    // read together, and waves with a head tile of their own need not be joined.  Sets of one: 64 rows of 8 heads
+    // 199 us for 180, 256 of 16 heads 327 for 80.
     const auto waste = [&](int64_t n) { return (p.head_tiles + n - 1) / n * n - p.head_tiles; };
     p.set_tiles = waves_of(p.dp, p.ht, p.mode);
     while (4 * waste(p.set_tiles) > p.head_tiles + waste(p.set_tiles))
@@ -1205,7 +1220,8 @@ void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
     else
         launch_tiles<DT, 256, 1>(a, grid, p.mode, st);
     if (p.shares) {
-        // few heads: their dims in slices of 32, so that more workgroups share the parts
+        // Few heads: their dims in slices of 32, so that more workgroups share the parts.  One row of 28 heads 55 us,
+        // by k_join4 85; 2048 heads 180 us, each in slices 189.
         const unsigned heads = (unsigned)(a.rows * a.heads * a.group);
         const unsigned fours = (unsigned)(a.rows * ((a.heads * a.group + 3) / 4));
         if (heads < 512)

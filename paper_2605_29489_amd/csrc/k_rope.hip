@@ -247,9 +247,8 @@ hipError_t launch(TurnArgs& a, int dtype, bool interleaved, int64_t heads, int64
     a.by_all = Div(a.all);
     a.by_per = Div((uint32_t)a.per);
     a.by_copy = Div((uint32_t)copy);
-    // as many tokens as there are threads for, fewer where that leaves CUs without a workgroup
-    int64_t tw = std::min<int64_t>(kThreads / a.all, (a.tokens + 511) / 512);
-    tw = std::max<int64_t>(1, std::min(tw, kMaxTurns / std::max(half, 1)));
+    // as many tokens as there are threads for
+    const int64_t tw = std::max<int64_t>(1, std::min<int64_t>(kThreads / a.all, kMaxTurns / std::max(half, 1)));
     a.tw = (int)tw;
     const size_t lds = (size_t)(tw * half) * sizeof(float2) + (size_t)tw * sizeof(int64_t);
     const unsigned grid = (unsigned)std::min<int64_t>((a.tokens + tw - 1) / tw, 1 << 20);

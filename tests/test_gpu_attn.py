@@ -437,7 +437,9 @@ def test_attend_pages_outside_the_cache_and_lengths_out_of_range(mp, dtype, page
     q = _dev(rng.standard_normal((6, H, dim)), dtype)
     out, lse = torch.empty_like(q), torch.empty(6, H, device="cuda")
     L = torch.tensor(lens, dtype=torch.int32, device="cuda")
-    mp.mp_kv_attend(c, q, torch.from_numpy(table).cuda(), L, out, lse=lse)
+    wide = torch.full((6, width + 3), 1, dtype=torch.int32, device="cuda")  # rows of a wider table
+    wide[:, :width] = torch.from_numpy(table).cuda()
+    mp.mp_kv_attend(c, q, wide[:, :width], L, out, lse=lse)
     torch.cuda.synchronize()
     Q = _host(q).reshape(6, heads, group, dim)
     for i, n in enumerate(lens):
@@ -714,6 +716,45 @@ def test_another_stream(mp):
         run()
     s.synchronize()
     assert all(_equal(a, b) for a, b in zip(outs, want))
+
+
+def test_two_streams_at_once(mp):
+    import torch
+    steps = [_step(mp, np.random.default_rng(s), longest=1000 * s + 7) for s in (1, 2)]
+    for run, aim, *_ in steps:
+        aim()
+        run()
+    torch.cuda.synchronize()
+    want = [[t.clone() for t in outs] for *_, outs in steps]
+    streams = [torch.cuda.Stream() for _ in steps]
+    for *_, outs in steps:
+        for t in outs[:3]:
+            t.fill_(-1)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (run, *_), s in zip(steps, streams):
+            run(stream=s)
+    torch.cuda.synchronize()
+    for (*_, outs), w in zip(steps, want):
+        assert all(_equal(a, b) for a, b in zip(outs, w))
+
+
+def test_no_rows_and_a_cache_without_pages(mp):
+    import torch
+    z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d, device="cuda")  # noqa: E731
+    c, e = mp.KvCache(z(2, 16, 2, 64), z(2, 16, 2, 64)), mp.KvCache(z(0, 16, 2, 64), z(0, 16, 2, 64))
+    none = z(0, d=torch.int64)
+    f = mp.mp_rope_frequencies(64)[0].cuda()
+    mp.mp_rope(z(0, 2, 64), z(0, 2, 64), none, f)
+    mp.mp_rope(z(3, 0, 64), z(3, 0, 64), z(3, d=torch.int64), f)
+    mp.mp_kv_append(c, z(0, 2, 64), z(0, 2, 64), none, positions=none, freqs=f, q=z(0, 4, 64))
+    mp.mp_kv_attend(c, z(0, 4, 64), z(0, 5, d=torch.int32), z(0, d=torch.int32), z(0, 4, 64))
+    # new tokens beside a cache that holds none: queries are turned, nothing is stored
+    q, at = torch.randn(3, 4, 64, device="cuda").bfloat16(), torch.arange(3, device="cuda")
+    want = torch.empty_like(q)
+    mp.mp_rope(q, want, at, f)
+    mp.mp_kv_append(e, q[:, :2].contiguous(), q[:, 2:].contiguous(), at, positions=at, freqs=f, q=q)
+    assert _equal(q, want)
 
 
 def test_graph_capture_and_replays_at_other_lengths(mp):
