@@ -262,12 +262,19 @@ def _floats(xs, K):
     return (C.c_float * K)(*xs)
 
 
+@functools.lru_cache(maxsize=None)
+def _raw_stream():
+    """torch's call for the current stream's handle alone (0.3 us against 3), and that for the current device."""
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle alone: 0.3 us against 3
+        raw, device = _raw_stream()
         if raw is not None:
-            return raw(torch.cuda.current_device())
+            return raw(device())
+        import torch
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return C.c_void_p(stream)
@@ -628,6 +635,12 @@ def mp_moe_workspace(layer: MoeLayer, dtype: int, tokens: int) -> int:
 
 
 # ------------------------------------------------------------------ attention over a paged cache
+@functools.lru_cache(maxsize=None)
+def _ints():
+    import torch
+    return torch.int32, torch.int64, torch.float64
+
+
 def _heads(t, shape, dtype, name: str):
     """Checks [tokens, heads, dim] values of unit stride inside a head; (token stride, head stride)."""
     if t.shape != shape:
@@ -642,8 +655,12 @@ def _heads(t, shape, dtype, name: str):
 
 def _head_rows(t, shape, dtype, name: str) -> int:
     """The same with the heads of a token side by side; its token stride."""
-    st, sh = _heads(t, shape, dtype, name)
     tokens, heads, dim = shape
+    if t.shape == shape and t.dtype is dtype:
+        st, sh, sd = t.stride()
+        if sd == 1 and sh == dim and tokens > 1:
+            return st
+    st, sh = _heads(t, shape, dtype, name)
     if sh != dim and heads > 1:
         raise ValueError(f"{name}: the heads of a token must be adjacent")
     return st if tokens > 1 else max(st, heads * dim)
@@ -653,12 +670,12 @@ def _turn_args(tokens, positions, freqs) -> int:
     """Checks them; the number of turned values of a head."""
     if freqs is None:
         return 0
-    import torch
+    _, i64, f64 = _ints()
     pairs = freqs.numel()
-    _vector(freqs, pairs, torch.float64, "freqs")
+    _vector(freqs, pairs, f64, "freqs")
     if positions is None:
         raise ValueError("freqs need positions")
-    _vector(positions, tokens, torch.int64, "positions")
+    _vector(positions, tokens, i64, "positions")
     return 2 * pairs
 
 
@@ -728,13 +745,12 @@ def mp_kv_append(cache: KvCache, k, v, slots, positions=None, freqs=None, q=None
     cache at ``slots`` (int64 [tokens], page * page_size + place; outside the cache: not stored), and the tokens'
     queries ``q`` [tokens, q_heads, dim], turned, in ``q_out`` (default: in place).  Without ``freqs`` nothing is
     turned."""
-    import torch
-    dt, (T, *heads), (_, _, *held) = cache._dtype, k.shape, cache._shape
-    if heads != held:
-        raise ValueError(f"k: heads {heads}, the cache's are {held}")
-    shape = (T, *heads)
+    dt, shape, held = cache._dtype, k.shape, cache._shape
+    T, heads = shape[0], shape[1:]
+    if heads != held[2:]:
+        raise ValueError(f"k: heads {tuple(heads)}, the cache's are {tuple(held[2:])}")
     ldk, ldv = _head_rows(k, shape, dt, "k"), _head_rows(v, shape, dt, "v")
-    _vector(slots, T, torch.int64, "slots")
+    _vector(slots, T, _ints()[1], "slots")
     rot = _turn_args(T, positions, freqs)
     hq = ldq = ldqo = 0
     if q is None:
@@ -762,13 +778,13 @@ def mp_kv_attend(cache: KvCache, q, table, lens, out, scale: Optional[float] = N
     ``scale``: of the scores, default dim^-0.5; ``window``: keys to look back, the token's own among them (0: all);
     ``lse``: fp32 [rows, q_heads], receives the log of the summed exponentials; ``workspace``: a device tensor of
     ``mp_kv_attend_workspace`` bytes to reuse between calls (default: a new one)."""
-    import torch
+    i32 = _ints()[0]
     dt, D = cache._dtype, cache._shape[3]
     R, H = q.shape[:2]
     shape = (R, H, D)
     ldq, ldo = _head_rows(q, shape, dt, "q"), _head_rows(out, shape, dt, "out")
     wide = table.shape
-    if len(wide) != 2 or wide[0] != R or table.dtype is not torch.int32:
+    if len(wide) != 2 or wide[0] != R or table.dtype is not i32:
         raise ValueError(f"table: shape {tuple(wide)} {table.dtype}, expected int32 of {R} rows")
     W = wide[1]
     st, sc = table.stride()
@@ -776,8 +792,9 @@ def mp_kv_attend(cache: KvCache, q, table, lens, out, scale: Optional[float] = N
         raise ValueError("table: the pages of a row must be adjacent")
     if R > 1 and st != 0 and st < W:
         raise ValueError(f"table: rows overlap or run backwards (stride {st})")
-    _vector(lens, R, torch.int32, "lens")
+    _vector(lens, R, i32, "lens")
     if lse is not None:
+        import torch
         if lse.shape != (R, H):
             raise ValueError(f"lse: shape {tuple(lse.shape)}, expected {(R, H)}")
         _vector(lse, R * H, torch.float32, "lse")
