@@ -198,6 +198,30 @@ def test_rope_non_finite_values_stay_in_their_pairs(mp):
         assert torch.equal(~torch.isfinite(y).cpu(), bad)
 
 
+@pytest.mark.parametrize("outer", ["tokens", "heads"])
+def test_rope_past_four_gib(mp, outer):
+    """Tokens, or heads, far apart: offsets past 32 bits, in bytes and in elements."""
+    import torch
+    rng = np.random.default_rng(4)
+    T, H, dim, stride = 3, 3, 64, 2 ** 31 + 8  # elements: the third is 8 GiB away
+    far = (stride, dim, 1) if outer == "tokens" else (dim, stride, 1)
+    try:
+        x = torch.zeros(2 * stride + 3 * dim, dtype=torch.bfloat16, device="cuda").as_strided((T, H, dim), far)
+    except torch.OutOfMemoryError:
+        pytest.skip("not enough device memory")
+    x.copy_(_dev(rng.standard_normal((T, H, dim)), "bf16"))
+    near, pos, f = x.clone(memory_format=torch.contiguous_format), torch.arange(5, 5 + T, device="cuda"), _freqs(dim)
+    f = torch.from_numpy(f).cuda()
+    want, y = torch.empty_like(near), torch.empty_like(near)
+    mp.mp_rope(near, want, pos, f)
+    mp.mp_rope(x, y, pos, f)
+    assert _equal(y, want)
+    back = torch.empty_like(near)
+    mp.mp_rope_backward(near, back, pos, f)
+    mp.mp_rope_backward(x, x, pos, f)
+    assert _equal(x, back)
+
+
 # ------------------------------------------------------------------ the cache
 def _new_cache(mp, dtype, pages, page, heads, dim, layout, rng=None):
     """A cache of NaN (or values) in one of the layouts."""
@@ -280,6 +304,25 @@ def test_append(mp, dtype, tokens, heads, group, dim, rot, inter, page, layout, 
         whole = t._base if t._base is not None else t
         both = 2 if layout in ("together", "braided") else 1
         assert int((~torch.isnan(whole)).sum()) == len(kept) * heads * dim * both
+
+
+def test_append_slots_named_twice(mp):
+    """Of tokens with one slot each value is one of theirs, key and value alike, and nothing else is written."""
+    import torch
+    rng = np.random.default_rng(8)
+    pages, page, heads, dim, tokens = 5, 7, 3, 72, 400
+    for dtype in ("bf16", "f32"):
+        c = _new_cache(mp, dtype, pages, page, heads, dim, "gaps")
+        at = rng.integers(0, 20, tokens)
+        k, v = (_dev(rng.standard_normal((tokens, heads, dim)), dtype) for _ in range(2))
+        mp.mp_kv_append(c, k, v, torch.from_numpy(at).cuda())
+        for got, new in ((_host(c.k), _host(k)), (_host(c.v), _host(v))):
+            flat = got.reshape(pages * page, heads, dim)
+            for slot in range(pages * page):
+                if (at == slot).any():
+                    assert (flat[slot] == new[at == slot]).any(0).all()
+                else:
+                    assert np.isnan(flat[slot]).all()
 
 
 # ------------------------------------------------------------------ attention
@@ -447,6 +490,28 @@ def test_attend_pages_outside_the_cache_and_lengths_out_of_range(mp, dtype, page
         _near(out[i], w[0].reshape(H, dim), w[2].reshape(H, dim), f"out {i}")
         _near(lse[i], w[1].reshape(H), w[3].reshape(H), f"lse {i}")
     assert (out[[1, 5]] == 0).all() and torch.isneginf(lse[[1, 5]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_pages_named_twice(mp, dtype):
+    """A page counts as often as a row names it, and rows may share pages."""
+    import torch
+    rng = np.random.default_rng(31)
+    pages, page, heads, group, dim = 6, 16, 2, 3, 64
+    lens = [150, 150, 40, 0, 97]
+    table = np.array([[2] * 10, [0, 1, 2, 3, 4, 5, 0, 1, 2, 3], [2, 2, 0, 0, 0, 0, 0, 0, 0, 0], [5] * 10,
+                      [4, 4, 4, 1, 1, 1, 4, 0, 0, 0]], np.int32)
+    c = _new_cache(mp, dtype, pages, page, heads, dim, "heads")
+    K, V = _fill(rng, c, np.arange(pages, dtype=np.int32)[None], [pages * page], page)
+    q = _dev(rng.standard_normal((len(lens), heads * group, dim)), dtype)
+    out, lse = torch.empty_like(q), torch.empty(len(lens), heads * group, device="cuda")
+    mp.mp_kv_attend(c, q, torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), out,
+                    lse=lse)
+    Q = _host(q).reshape(len(lens), heads, group, dim)
+    for i, n in enumerate(lens):
+        w = _attention(Q[i], K, V, _slots(table[i], n, page, 0, pages), dim ** -0.5, dtype)
+        _near(out[i], w[0].reshape(-1, dim), w[2].reshape(-1, dim), f"row {i}")
+        _near(lse[i], w[1].reshape(-1), w[3].reshape(-1), f"row {i}")
 
 
 @pytest.mark.parametrize("heads,dim,rows,n", [(16, 64, 20, 500), (8, 128, 40, 300), (2, 128, 1, 9000),
@@ -782,6 +847,44 @@ def test_graph_capture_and_replays_at_other_lengths(mp):
         run()
         torch.cuda.synchronize()
         assert all(_equal(a, b) for a, b in zip(outs, got)), i
+
+
+def test_two_graphs_that_share_a_workspace(mp):
+    """Captured on one stream and replayed in turn, with other lengths and eager calls between: each call leaves the
+    workspace to the next."""
+    import torch
+    rng = np.random.default_rng(12)
+    page, heads, group, dim, H = 16, 2, 4, 128, 8
+    pages = 700
+    c = _new_cache(mp, "bf16", pages, page, heads, dim, "tokens")
+    c.k.copy_(torch.randn(c.k.shape, device="cuda"))
+    c.v.copy_(torch.randn(c.v.shape, device="cuda"))
+    calls = []
+    for rows, width in ((5, 120), (1, 600)):
+        table = torch.from_numpy(rng.integers(0, pages, (rows, width)).astype(np.int32)).cuda()
+        q = _dev(rng.standard_normal((rows, H, dim)), "bf16")
+        calls.append((q, table, torch.full((rows,), 9, dtype=torch.int32, device="cuda"), torch.empty_like(q)))
+    ws = torch.empty(max(mp.mp_kv_attend_workspace(c, len(q), H, t.shape[1]) for q, t, *_ in calls),
+                     dtype=torch.uint8, device="cuda")
+    graphs = []
+    for q, table, lens, out in calls:
+        mp.mp_kv_attend(c, q, table, lens, out, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            mp.mp_kv_attend(c, q, table, lens, out, workspace=ws)
+    for turn in range(4):
+        for (q, table, lens, out) in calls:
+            lens.copy_(torch.from_numpy(rng.integers(0, table.shape[1] * page + 1, len(q)).astype(np.int32)))
+            out.fill_(-1)
+        torch.cuda.synchronize()
+        for g in graphs if turn % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for q, table, lens, out in calls:
+            want = torch.empty_like(out)
+            mp.mp_kv_attend(c, q, table, lens, want)
+            assert _equal(out, want), turn
 
 
 def test_refusals_of_device_buffers(mp):
