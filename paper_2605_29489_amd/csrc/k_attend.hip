@@ -183,7 +183,7 @@ __device__ inline bool find_share(const AttendArgs& a, uint32_t number, Share* o
     // a share holds kMinTiles at least, but no more than a row has where rows are
     // short: 132 of 1 tile (fp32) 21.5 us in shares of 4 and 9.6 of 1
     const uint32_t row = (uint32_t)min(quotient(total + a.rows - 1, (uint32_t)a.rows), (uint64_t)kMinTiles);
-    out->per = even < row ? row : even < 0x7fffffff ? (uint32_t)even : 0x7fffffffu;
+    out->per = max((uint32_t)even, row);  // all < 2^38
     out->at = (uint64_t)number * out->per;
     out->end = min(all, out->at + out->per);
     out->row = 0;
@@ -1179,7 +1179,11 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     const int64_t tiles = (most + tile - 1) / tile + (slides ? 1 : 0);  // a window may begin inside a tile
     // a launch takes fewer than 2^32 threads along x
     const int64_t threads = s.rows * p.head_tiles * 64 * waves_of(p.dp, p.ht, p.mode);
-    if (tiles > kMinTiles || threads >= (int64_t)1 << 32)
+    // A share counts its tiles in 31 bits.  Tables with room for more have 2^13 rows and head sets or more, which
+    // fill the chip unsplit; and no 2^22, whose threads would be too many: rows * q_heads <= 2^23, and a set holds two
+    // head tiles or more where a row has that many.
+    const int64_t all = s.rows * ((p.head_tiles + p.set_tiles - 1) / p.set_tiles) * tiles;
+    if (all < (int64_t)1 << 38 && (tiles > kMinTiles || threads >= (int64_t)1 << 32))
         p.shares = std::min<int64_t>(kShares, (s.rows * p.head_tiles * tiles + kMinTiles - 1) / kMinTiles);
     else if (p.one_if_few)
         p.set_tiles = 1;

@@ -156,6 +156,21 @@ def test_attend_shapes_refused(mp, over):
     assert mp.lib.mp_kv_attend_workspace(C.byref(c), C.byref(s), None) == mp.MP_E_ARG
 
 
+@pytest.mark.parametrize("dtype,rows,q_heads,width", [
+    ("MP_BF16", 1 << 14, 1, 1 << 25), ("MP_F32", 1 << 13, 1, 1 << 25), ("MP_BF16", 1 << 20, 8, 1 << 19),
+    ("MP_F32", 1 << 18, 16, 1 << 20)])
+def test_tables_with_room_for_more_tiles_than_a_share_counts(mp, dtype, rows, q_heads, width):
+    """2^38 tiles (of 32 keys, fp32 16) would be 256 shares of 2^30: rows are not split then, and need no workspace."""
+    def need(rows, width):
+        n = C.c_uint64(7)
+        c = _cache(mp, dtype=getattr(mp, dtype), heads=1, head_dim=128, page_stride=2048, slot_stride=128)
+        s = _attend(mp, rows=rows, q_heads=q_heads, width=width, ldq=2048, ldo=2048, ldt=0)
+        assert mp.lib.mp_kv_attend_workspace(C.byref(c), C.byref(s), C.byref(n)) == mp.MP_OK
+        return n.value
+    assert need(rows, width) == 0
+    assert need(rows - 1, width) > 0 and need(rows, width - 2) > 0
+
+
 def test_no_rows_no_tokens(mp):
     c, r, s = _cache(mp), _rows(mp, tokens=0), _attend(mp, rows=0)
     assert mp.lib.mp_kv_append(C.byref(c), C.byref(r), None, None, None, None, None, None, None, None) == mp.MP_OK

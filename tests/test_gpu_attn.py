@@ -560,6 +560,30 @@ def test_attend_many_rows_of_one_sequence(mp):
     assert not torch.isnan(out).any() and torch.equal(torch.isneginf(lse).all(1), lens == 0)
 
 
+def test_attend_short_rows_of_a_very_wide_table(mp):
+    """A table row of 2^25 pages for 2^14 rows: room for so many keys that rows are not split."""
+    import torch
+    rng = np.random.default_rng(6)
+    rows, width, group, dim, page = 1 << 14, 1 << 25, 3, 128, 16
+    c = _new_cache(mp, "bf16", 300, page, 1, dim, "tokens")
+    named = rng.integers(0, 300, 320).astype(np.int32)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, :320] = torch.from_numpy(named).cuda()
+    K, V = _fill(rng, c, np.arange(300, dtype=np.int32)[None], [300 * page], page)
+    q = torch.randn(rows, group, dim, dtype=torch.bfloat16, device="cuda")
+    lens = (torch.arange(rows, device="cuda") % 71).int()
+    lens[5], lens[9000] = 5000, 4113
+    assert mp.mp_kv_attend_workspace(c, rows, group, width) == 0
+    out, lse = torch.full_like(q, float("nan")), torch.full((rows, group), float("nan"), device="cuda")
+    mp.mp_kv_attend(c, q, table.expand(rows, -1), lens, out, lse=lse)
+    torch.cuda.synchronize()
+    for i in [0, 1, 5, 70, 71, 4095, 9000, rows - 1]:
+        w = _attention(_host(q[i])[None], K, V, _slots(named, int(lens[i]), page, 0, 300), dim ** -0.5, "bf16")
+        _near(out[i], w[0][0], w[2][0], f"out {i}")
+        _near(lse[i], w[1][0], w[3][0], f"lse {i}")
+    assert not torch.isnan(out).any() and torch.equal(torch.isneginf(lse).all(1), lens == 0)
+
+
 def test_attend_splits_do_not_change_what_a_row_is(mp):
     """A row alone, among others and cut in two that lse joins: within the tolerance of each other."""
     import torch
