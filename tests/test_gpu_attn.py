@@ -222,6 +222,34 @@ def test_rope_past_four_gib(mp, outer):
     assert _equal(x, back)
 
 
+def test_more_tokens_than_workgroups(mp):
+    """A million tokens of many heads, for workgroups that take several: as in calls of a part of them each."""
+    import torch
+    T, heads, dim = (1 << 20) + 777, 127, 2
+    x = torch.randn(T, heads + 2, dim, device="cuda").bfloat16()
+    pos, f = torch.arange(T, device="cuda") * 3, torch.tensor([0.7], dtype=torch.float64, device="cuda")
+    y, want = torch.empty_like(x), torch.empty_like(x)
+    mp.mp_rope(x, y, pos, f)
+    for a in range(0, T, 1 << 18):
+        b = min(a + (1 << 18), T)
+        mp.mp_rope(x[a:b], want[a:b], pos[a:b], f)
+    assert _equal(y, want)
+    q, k, v = torch.split(x, (heads, 1, 1), 1)
+    pages, page = T // 7 + 1, 7
+    c = mp.KvCache(*(torch.full((pages, page, 1, dim), float("nan"), dtype=torch.bfloat16, device="cuda")
+                     for _ in range(2)))
+    slots = torch.randperm(pages * page, device="cuda")[:T]
+    slots[::1000] = -1
+    q_out = torch.empty(T, heads, dim, dtype=torch.bfloat16, device="cuda")
+    mp.mp_kv_append(c, k, v, slots, positions=pos, freqs=f, q=q, q_out=q_out)
+    assert _equal(q_out, want[:, :heads])
+    kept = slots >= 0
+    for got, new in ((c.k, want[:, heads:heads + 1]), (c.v, v)):
+        flat = got.view(pages * page, 1, dim)
+        assert _equal(flat[slots[kept]], new[kept])
+        assert int((~torch.isnan(flat)).sum()) == int(kept.sum()) * dim
+
+
 # ------------------------------------------------------------------ the cache
 def _new_cache(mp, dtype, pages, page, heads, dim, layout, rng=None):
     """A cache of NaN (or values) in one of the layouts."""
