@@ -1173,10 +1173,11 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     while (4 * waste(p.set_tiles) > p.head_tiles + waste(p.set_tiles))
         p.set_tiles /= 2;
     p.one_if_few = s.rows * p.head_tiles < kShares;
-    int64_t most = s.width * c.page_size;
+    const auto tiles_in = [&](int64_t keys) { return (keys + tile - 1) / tile; };
+    const int64_t most = s.width * c.page_size;
+    // a window may begin inside a tile, but a row has no more than its table has room for
     const bool slides = s.window > 0 && s.window < most;
-    most = slides ? s.window : most;
-    const int64_t tiles = (most + tile - 1) / tile + (slides ? 1 : 0);  // a window may begin inside a tile
+    const int64_t tiles = slides ? std::min(tiles_in(s.window) + 1, tiles_in(most)) : tiles_in(most);
     // a launch takes fewer than 2^32 threads along x
     const int64_t threads = s.rows * p.head_tiles * 64 * waves_of(p.dp, p.ht, p.mode);
     // A share counts its tiles in 31 bits.  Tables with room for more have 2^13 rows and head sets or more, which

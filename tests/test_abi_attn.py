@@ -171,6 +171,29 @@ def test_tables_with_room_for_more_tiles_than_a_share_counts(mp, dtype, rows, q_
     assert need(rows - 1, width) > 0 and need(rows, width - 2) > 0
 
 
+def _need(mp, rows, q_heads, width, window, **cache):
+    n = C.c_uint64(7)
+    c, s = _cache(mp, **cache), _attend(mp, rows=rows, q_heads=q_heads, width=width, window=window)
+    assert mp.lib.mp_kv_attend_workspace(C.byref(c), C.byref(s), C.byref(n)) == mp.MP_OK
+    return n.value
+
+
+@pytest.mark.parametrize("dtype,tile", [("MP_BF16", 32), ("MP_F32", 16)])
+@pytest.mark.parametrize("page", [1, 10, 16, 64])
+@pytest.mark.parametrize("rows,q_heads", [(1, 2), (4, 8), (64, 14), (5000, 2)])
+def test_a_window_takes_no_more_workspace_than_every_key(mp, dtype, tile, page, rows, q_heads):
+    """A window counts no more tiles than the table has room for: four tiles are not split, with or without one."""
+    cache = dict(dtype=getattr(mp, dtype), page_size=page, page_stride=16 * page)
+    for most in (page, 3 * tile, 4 * tile - 1, 4 * tile, 4 * tile + 1, 9 * tile, 300 * tile):
+        width = max(1, most // page)
+        most = width * page
+        whole = _need(mp, rows, q_heads, width, 0, **cache)
+        assert (whole == 0) == (most <= 4 * tile)
+        for window in {1, 2, most // 2, most - tile, most - 2, most - 1, most, most + 1, 2 * most, 1 << 40}:
+            if window > 0:
+                assert _need(mp, rows, q_heads, width, window, **cache) <= whole, (most, window)
+
+
 def test_no_rows_no_tokens(mp):
     c, r, s = _cache(mp), _rows(mp, tokens=0), _attend(mp, rows=0)
     assert mp.lib.mp_kv_append(C.byref(c), C.byref(r), None, None, None, None, None, None, None, None) == mp.MP_OK
