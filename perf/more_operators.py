@@ -264,7 +264,7 @@ def _own(s):
     if s["op"] == "attend":
         kv = mp.KvCache(s["k"], s["v"])
         if "workspace" not in s:
-            need = mp.mp_kv_attend_workspace(kv, s["q"].shape[0], s["q"].shape[1], s["table"].shape[1])
+            need = mp.mp_kv_attend_workspace(kv, s["q"].shape[0], s["q"].shape[1], s["table"].shape[1], s["window"])
             s["workspace"] = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
         mp.mp_kv_attend(kv, s["q"], s["table"], s["lens"], s["out"], scale=s["scale"], window=s["window"],
                         lse=s["stat"], workspace=s["workspace"])
