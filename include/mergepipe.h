@@ -576,8 +576,9 @@ typedef struct mp_rope_shape {
  *   positions: device int64[tokens], of any sign, |position| < 2^52; freqs:
  *   device double[rot_dim / 2], radians per position (mp_rope_frequencies).
  *   y may be x itself (same pointer and strides).
- * Angles are formed in 64 bits, reduced to a turn, and their sine and cosine
- * taken in 32, so that far positions lose nothing. */
+ * Angles are formed and reduced to a turn in 64 bits, off by less than
+ * |position freq| 2^-51 radians, and their sine and cosine rounded to 32: an
+ * fp32 value does not show it up to positions of some 2^26. */
 int mp_rope(const mp_rope_shape* shape, const void* x, const int64_t* positions, const double* freqs, void* y,
             void* stream);
 

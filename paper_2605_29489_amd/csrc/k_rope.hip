@@ -9,15 +9,20 @@ namespace {
 
 // cos and sin of pos * f, times the amplitude.  The angle is taken in turns and
 // in 64 bits, where subtracting the nearest whole turn is exact: what is left,
-// at most half a turn, is off by pos f 2^-54 or so and is then rounded to fp32,
-// 2^-26 of a turn at most.
+// at most half a turn, is off by 3 |pos f| 2^-53 / 2 pi.  Its fp32 value h is up
+// to 2^-25 half turns away; that rest l is added to first order, sin(h + l) =
+// sin h + l cos h and so on, whose next term is under 2^-47.  It costs nothing
+// that can be measured; sincospi in 64 bits takes 8192 appended tokens of 32 + 8
+// heads from 40 us to 48.
 __device__ inline float2 turn_of(int64_t pos, double f, float amp)
 {
     double t = (double)pos * (f * 0.15915494309189533577);
     t -= rint(t);
+    t += t;
+    const float h = (float)t, l = (float)(t - h) * 3.14159265358979f;
     float s, c;
-    sincospif((float)(t + t), &s, &c);
-    return make_float2(c * amp, s * amp);
+    sincospif(h, &s, &c);
+    return make_float2(fmaf(-l, s, c) * amp, fmaf(l, c, s) * amp);
 }
 
 // Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and

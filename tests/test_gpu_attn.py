@@ -185,6 +185,30 @@ def test_rope_gradient_against_the_formula_and_differences(mp):
                 assert abs(got - _host(dx[t, 1, j])) <= 4 * (TURN + 4 * EPS) * mag * np.abs(_host(dy[t, 1])).sum()
 
 
+@pytest.mark.parametrize("inter", [False, True])
+def test_rope_small_cosines_and_sines_keep_their_bits(mp, inter):
+    """Angles near a quarter and a half turn that lie between two fp32 values: of a pair (1, 0), cos and sin themselves.
+    Each is right to 4 units of 2^-23 for the function and half a unit for each of its two roundings, relative to it;
+    what is added to first order leaves 2^-48 + 2^-25 pi (4.5 2^-23 + 2^-23), less than 2^-43."""
+    import torch
+    half = 64
+    j = np.arange(1, half + 1)
+    for centre in (0.5, 1.0):  # half turns
+        for sign in (1, -1):
+            turns = sign * (centre - j * 2.0 ** -20 - 0.45 * 2.0 ** -24)
+            f = turns * math.pi
+            x = torch.zeros(2, 1, 2 * half, device="cuda")
+            a, b = (slice(0, None, 2), slice(1, None, 2)) if inter else (slice(0, half), slice(half, None))
+            x[:, :, a] = 1.0
+            y = torch.empty_like(x)
+            mp.mp_rope(x, y, torch.tensor([1, -1], device="cuda"), torch.from_numpy(f).cuda(), interleaved=inter)
+            for t, pos in enumerate((1, -1)):
+                w = (np.longdouble(pos) * f.astype(np.longdouble))
+                for got, want in ((y[t, 0, a], np.cos(w)), (y[t, 0, b], np.sin(w))):
+                    want = want.astype(float)
+                    _near(got, want, 5 * EPS * np.abs(want) + 2.0 ** -43, f"centre {centre}, position {pos}")
+
+
 def test_rope_non_finite_values_stay_in_their_pairs(mp):
     import torch
     for dtype in ("bf16", "f32"):
