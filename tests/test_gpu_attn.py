@@ -512,6 +512,34 @@ def test_attend(mp, dtype, lens, heads, group, dim, page, layout, window):
     assert _equal(q, first)
 
 
+ATTEND_FORMS = [  # the same: groups of more than 16 heads in every kind of page and head size, heads of few values
+    ([300, 5], 2, 17, 72, 10, "tokens", 0),
+    ([2500, 1], 1, 33, 48, 10, "gaps", 0),
+    ([300, 31], 2, 20, 96, 16, "heads", 0),
+    ([300, 31], 1, 24, 24, 16, "tokens", 0),
+    ([2100, 40, 0], 2, 40, 112, 48, "gaps", 0),
+    ([700, 90, 1], 3, 19, 128, 7, "together", 200),
+    ([40, 3, 0, 150] * 70, 8, 17, 64, 5, "tokens", 0),
+    ([260, 31] * 20, 8, 18, 80, 16, "heads", 0),
+    ([3000, 17], 2, 3, 3, 10, "tokens", 0),
+    ([700, 5], 1, 20, 3, 16, "tokens", 0),
+    ([90] * 300, 8, 1, 7, 16, "tokens", 0),
+    ([260, 0, 200] * 25, 8, 1, 3, 16, "heads", 0),
+    ([2000], 3, 2, 2, 16, "braided", 0),
+    ([1500, 3], 2, 5, 5, 7, "gaps", 300),
+    ([900, 0, 1], 1, 33, 1, 16, "tokens", 0),
+    ([1200, 77], 2, 40, 7, 10, "gaps", 0),
+    ([96, 5, 90, 33], 2, 4, 128, 16, "tokens", 127),  # a window of almost all the table's four tiles
+    ([96, 5, 90, 33], 2, 4, 128, 16, "tokens", 70),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,heads,group,dim,page,layout,window", ATTEND_FORMS)
+def test_attend_every_form(mp, dtype, lens, heads, group, dim, page, layout, window):
+    test_attend(mp, dtype, lens, heads, group, dim, page, layout, window)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("page,group", [(16, 4), (10, 4), (64, 17)])
 def test_attend_pages_outside_the_cache_and_lengths_out_of_range(mp, dtype, page, group):
