@@ -104,8 +104,9 @@ def main(prompt=96, steps=8, sequences=4, seed=0, say=print):
 
     # rotary positions alone, as training takes them: <turned q, d> = <q, d turned back>
     q = block.project(x)[0].contiguous()
-    d, turned, back = rand(*q.shape), torch.empty_like(q), torch.empty_like(q)
+    turned, back = torch.empty_like(q), torch.empty_like(q)
     mp.mp_rope(q, turned, at, block.freqs)
+    d = turned + rand(*q.shape)  # so that both sides are of the products' size
     mp.mp_rope_backward(d, back, at, block.freqs)
     dots = [float((a.double() * b.double()).sum()) for a, b in ((turned, d), (q, back))]
     scale = float((q.double() * d.double()).abs().sum())

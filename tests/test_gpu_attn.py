@@ -1051,3 +1051,59 @@ def test_example_serves_a_merge(mp):
     # each of the two sums of products of bf16 values carries the roundings of its turned factor, 2^-8 at most, and of
     # the turn itself; a pair's products are at most twice those of the untouched values
     assert abs(dots[0] - dots[1]) <= 2 * 2 * (2.0 ** -8 + 2 * TURN) * 2 * scale
+
+
+def test_example_attends_to_its_own_tokens(mp, monkeypatch):
+    """Every append and attention of the example's eager steps against the tokens that its sequences have had: where a
+    position, slot, page or length were wrong, a row would be attended to other keys.  And the gradient of its rotary
+    positions value by value."""
+    import torch
+    from examples import decode
+    append, attend, backward = mp.mp_kv_append, mp.mp_kv_attend, mp.mp_rope_backward
+    tokens, calls, backs = [], [], []
+
+    def eager():
+        return not torch.cuda.is_current_stream_capturing()
+
+    def on_append(cache, k, v, slots, positions, freqs, q, **kw):
+        if eager():
+            tokens.append([t.clone() for t in (k, v, q, positions)] + [freqs, kw])
+        append(cache, k, v, slots, positions=positions, freqs=freqs, q=q, **kw)
+
+    def on_attend(cache, q, table, lens, out, **kw):
+        assert not kw  # the head's scale, every key
+        attend(cache, q, table, lens, out)
+        if eager():
+            calls.append([t.clone() for t in (q, table, lens, out)])
+
+    def on_backward(dy, dx, positions, freqs):
+        backward(dy, dx, positions, freqs)
+        backs.append((dy, dx, positions, freqs))
+    for name, f in (("mp_kv_append", on_append), ("mp_kv_attend", on_attend), ("mp_rope_backward", on_backward)):
+        monkeypatch.setattr(decode.mp, name, f)
+    prompt, sequences = 40, 3
+    decode.main(prompt=prompt, steps=2, sequences=sequences, say=lambda s: None)
+    assert len(tokens) == len(calls) == 1 + prompt + 1
+    history = {}
+    for (k, v, q0, pos, freqs, kw), (q, table, lens, out) in zip(tokens, calls):
+        assert set(kw) <= {"amplitude"}
+        keys, turned = torch.empty_like(k), torch.empty_like(q)
+        mp.mp_rope(k, keys, pos, freqs, **kw)
+        mp.mp_rope(q0, turned, pos, freqs, **kw)
+        assert _equal(q, turned)
+        H, heads, dim = q.shape[1], *k.shape[1:]
+        rows = [tuple(r) for r in table.tolist()]  # a sequence is known by its pages
+        for t, row in enumerate(rows):
+            past = history.setdefault(row, ([], []))
+            assert int(pos[t]) == len(past[0]) and int(lens[t]) == len(past[0]) + 1
+            past[0].append(_host(keys[t]))
+            past[1].append(_host(v[t]))
+        for t, row in enumerate(rows):
+            n = int(lens[t])
+            w = _attention(_host(q[t]).reshape(heads, H // heads, dim), np.stack(history[row][0][:n]),
+                           np.stack(history[row][1][:n]), np.arange(n), dim ** -0.5, "bf16")
+            _near(out[t], w[0].reshape(H, dim), w[2].reshape(H, dim), f"sequence {row}, token {n - 1}")
+    assert sorted(len(p[0]) for p in history.values()) == [1] * (sequences - 1) + [prompt, prompt + 1]
+    (dy, dx, pos, freqs), = backs
+    want, tol = _turn(_host(dy), _host(pos).astype(np.int64), _host(freqs), False, 1.0, back=True)
+    _near(dx, want, tol + U["bf16"] * 1.01 * np.abs(want), "the rotary gradient")
