@@ -722,17 +722,19 @@ def mp_rope_backward(dy, dx, positions, freqs, interleaved: bool = False, amplit
 
 
 class KvCache:
-    """mp_kv_cache: keys and values [pages, page_size, heads, dim], device tensors of the same type and strides in
-    which the values of a head are adjacent; they may be transposed views (heads before a page's tokens) and parts of
-    one array."""
+    """mp_kv_cache: keys and values [pages, page_size, heads, dim], device tensors of the same type and, but in
+    dimensions of one place, strides in which the values of a head are adjacent; they may be transposed views (heads
+    before a page's tokens) and parts of one array."""
 
     def __init__(self, k, v):
         shape, strides, dt = k.shape, k.stride(), k.dtype
         if len(shape) != 4 or shape != v.shape or dt is not v.dtype:
             raise ValueError(f"k {tuple(shape)} {dt}, v {tuple(v.shape)} {v.dtype}: expected two equal "
                              "[pages, page_size, heads, dim]")
-        if strides != v.stride() or (strides[3] != 1 and shape[3] > 1):
-            raise ValueError("k and v need equal strides, and adjacent values in a head")
+        if strides != v.stride() and any(a != b for n, a, b in zip(shape, strides, v.stride()) if n > 1):
+            raise ValueError("k and v need equal strides")
+        if strides[3] != 1 and shape[3] > 1:
+            raise ValueError("k and v: the values of a head must be adjacent")
         self.k, self.v = k, v
         self._shape, self._dtype = shape, dt
         self._s = mp_kv_cache(_code_of(dt), 0, *shape, *strides[:3], k.data_ptr(), v.data_ptr())

@@ -200,6 +200,18 @@ def test_no_rows_no_tokens(mp):
     assert mp.lib.mp_kv_attend(C.byref(c), C.byref(s), None, None, None, None, None, None, 0, None) == mp.MP_OK
 
 
+def test_a_cache_of_one_page_or_head_takes_any_strides_there(mp):
+    """Strides of a dimension of one place are no strides: a part of a larger array beside an array of its own."""
+    import torch
+    z = torch.zeros
+    for k, v in ((z(1, 16, 2, 8), z(3, 16, 2, 16)[1:2, :, :, :8].contiguous().as_strided((1, 16, 2, 8), (7, 16, 8, 1))),
+                 (z(4, 16, 1, 8), z(4, 16, 1, 8).as_strided((4, 16, 1, 8), (128, 8, 3, 1))),
+                 (z(4, 1, 2, 8), z(4, 1, 2, 8).as_strided((4, 1, 2, 8), (16, 99, 8, 1)))):
+        mp.KvCache(k, v)
+    with pytest.raises(ValueError):
+        mp.KvCache(z(2, 16, 2, 8), z(2, 16, 4, 8)[:, :, :2])
+
+
 def test_binding_refuses_shapes_and_types(mp):
     import torch
     z = torch.zeros

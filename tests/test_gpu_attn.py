@@ -1029,6 +1029,25 @@ def test_refusals_of_device_buffers(mp):
     torch.cuda.synchronize()
 
 
+def test_one_page_beside_an_array_of_many(mp):
+    """Keys in an array of their own, values in a page of a larger one whose stride differs."""
+    import torch
+    rng = np.random.default_rng(9)
+    k = torch.zeros(1, 16, 2, 64, device="cuda")
+    v = torch.zeros(3, 2, 16, 2, 64, device="cuda")[1:2, 1]
+    assert k.stride() != v.stride()
+    c = mp.KvCache(k, v)
+    new = [_dev(rng.standard_normal((16, 2, 64)), "f32") for _ in range(2)]
+    mp.mp_kv_append(c, new[0], new[1], torch.arange(16, device="cuda"))
+    assert _equal(k[0], new[0]) and _equal(v[0], new[1])
+    q = _dev(rng.standard_normal((1, 4, 64)), "f32")
+    out = torch.empty_like(q)
+    mp.mp_kv_attend(c, q, torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
+                    torch.tensor([13], dtype=torch.int32, device="cuda"), out)
+    w = _attention(_host(q).reshape(2, 2, 64), _host(new[0]), _host(new[1]), np.arange(13), 64 ** -0.5, "f32")
+    _near(out[0], w[0].reshape(4, 64), w[2].reshape(4, 64), "out")
+
+
 class _Null:
     """A tensor of another's shape at address 0."""
 
