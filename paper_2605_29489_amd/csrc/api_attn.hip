@@ -53,6 +53,45 @@ int check_values(Seen& seen, const void* p, int64_t n, int size, const char* nam
     return check_rows(seen, p, 1, n, n, size, name, out);
 }
 
+// Extents and strides (elements) of an array of heads, from the innermost on;
+// those of one place only are left out.
+struct Nest {
+    int64_t n[3], stride[3];
+    int k = 0;
+};
+
+Nest nest(const int64_t* n, const int64_t* stride, int count)
+{
+    Nest r;
+    for (int i = 0; i < count; ++i)
+        if (n[i] > 1) {
+            r.n[r.k] = n[i];
+            r.stride[r.k++] = stride[i];
+        }
+    for (int i = 1; i < r.k; ++i)
+        for (int j = i; j > 0 && r.stride[j] < r.stride[j - 1]; --j) {
+            std::swap(r.stride[j], r.stride[j - 1]);
+            std::swap(r.n[j], r.n[j - 1]);
+        }
+    return r;
+}
+
+// Whether heads of dim elements meet where one array starts d elements behind
+// the other: some difference of two places is less than dim from d.
+bool places_meet(const Nest& r, int k, __int128 d, int64_t dim)
+{
+    if (k == 0)
+        return d > -dim && d < dim;
+    // the strides inside this one, and a head, reach less far than it, so that
+    // only the two multiples beside d can come near it
+    const __int128 st = r.stride[k - 1], most = r.n[k - 1] - 1;
+    __int128 q = d / st;
+    for (__int128 m = q - 1; m <= q + 1; ++m)
+        if (m >= -most && m <= most && places_meet(r, k - 1, d - m * st, dim))
+            return true;
+    return false;
+}
+
 // ---------------------------------------------------------------- rotary positions
 int check_turn(int64_t dim, int64_t rot, int32_t flags, float amplitude)
 {
@@ -113,6 +152,14 @@ int check_heads(Seen& seen, const void* p, const mp_rope_shape& s, int64_t ld, i
     return check_rows(seen, p, rows, (int64_t)inner, outer_t ? ld : hd, es, name, out);
 }
 
+// Whether heads of a tensor share memory with those of one that starts d elements behind it.
+bool heads_meet(const mp_rope_shape& s, int64_t ld, int64_t hd, int64_t d)
+{
+    const int64_t n[2] = {s.tokens, s.heads}, st[2] = {ld, hd};
+    const Nest r = nest(n, st, 2);
+    return places_meet(r, r.k, d, s.head_dim);
+}
+
 int rope(const mp_rope_shape* shape, const void* in, const int64_t* positions, const double* freqs, void* out,
          bool back, void* stream)
 {
@@ -147,52 +194,23 @@ int rope(const mp_rope_shape* shape, const void* in, const int64_t* positions, c
         (s.rot_dim && (rc = check_values(seen, positions, s.tokens, 8, "positions", &P))) ||
         (s.rot_dim && (rc = check_values(seen, freqs, s.rot_dim / 2, 8, "freqs", &F))))
         return rc;
-    if ((rc = check_apart(Y, X, a.ldx == a.ldy && a.hdx == a.hdy)) || (rc = check_apart(Y, P, false)) ||
-        (rc = check_apart(Y, F, false)))
+    // where the strides are equal, heads of one may lie between those of the other
+    const bool alike = a.ldx == a.ldy && a.hdx == a.hdy;
+    const bool between = alike && X.s.p != Y.s.p && meet(Y.s, X.s) &&
+                         !heads_meet(s, a.ldx, a.hdx, (Y.s.p - X.s.p) / es);
+    if (!between && (rc = check_apart(Y, X, alike)))
+        return rc;
+    if ((rc = check_apart(Y, P, false)) || (rc = check_apart(Y, F, false)))
         return rc;
     const hipError_t e = launch_rope(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MP_OK : hip_fail(e, "rope launch");
 }
 
 // ---------------------------------------------------------------- the cache
-// Extents and strides (elements) of the cache's places, from the innermost on;
-// places of which there is one only are left out.
-struct Nest {
-    int64_t n[3], stride[3];
-    int k = 0;
-};
-
 Nest nest(const mp_kv_cache& c)
 {
-    Nest r;
     const int64_t n[3] = {c.pages, c.page_size, c.heads}, st[3] = {c.page_stride, c.slot_stride, c.head_stride};
-    for (int i = 0; i < 3; ++i)
-        if (n[i] > 1) {
-            r.n[r.k] = n[i];
-            r.stride[r.k++] = st[i];
-        }
-    for (int i = 1; i < r.k; ++i)
-        for (int j = i; j > 0 && r.stride[j] < r.stride[j - 1]; --j) {
-            std::swap(r.stride[j], r.stride[j - 1]);
-            std::swap(r.n[j], r.n[j - 1]);
-        }
-    return r;
-}
-
-// Whether heads of dim elements meet where one array starts d elements behind
-// the other: some difference of two places is less than dim from d.
-bool places_meet(const Nest& r, int k, __int128 d, int64_t dim)
-{
-    if (k == 0)
-        return d > -dim && d < dim;
-    // the strides inside this one, and a head, reach less far than it, so that
-    // only the two multiples beside d can come near it
-    const __int128 st = r.stride[k - 1], most = r.n[k - 1] - 1;
-    __int128 q = d / st;
-    for (__int128 m = q - 1; m <= q + 1; ++m)
-        if (m >= -most && m <= most && places_meet(r, k - 1, d - m * st, dim))
-            return true;
-    return false;
+    return nest(n, st, 3);
 }
 
 int check_cache(const mp_kv_cache* c, int* es)

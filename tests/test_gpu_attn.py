@@ -1029,6 +1029,31 @@ def test_refusals_of_device_buffers(mp):
     torch.cuda.synchronize()
 
 
+def test_rope_between_the_heads_of_its_input(mp):
+    """An output whose heads lie between the input's, of one token and of several, tokens outside heads and inside."""
+    import torch
+    rng = np.random.default_rng(2)
+    f = torch.from_numpy(_freqs(16)).cuda()
+    for T in (1, 5):
+        pos = torch.arange(3, 3 + T, device="cuda")
+        for inside in (False, True):
+            buf = _dev(rng.standard_normal((6, T, 16) if inside else (T, 6, 16)), "bf16")
+            x, y = (buf[0::2], buf[1::2]) if inside else (buf[:, 0::2], buf[:, 1::2])
+            if inside:
+                x, y = x.transpose(0, 1), y.transpose(0, 1)
+            kept, want = x.clone(), torch.empty(T, 3, 16, dtype=torch.bfloat16, device="cuda")
+            mp.mp_rope(kept.contiguous(), want, pos, f)
+            mp.mp_rope(x, y, pos, f)
+            assert _equal(y, want) and _equal(x, kept)
+            mp.mp_rope_backward(kept.contiguous(), want, pos, f)
+            mp.mp_rope_backward(x, y, pos, f)
+            assert _equal(y, want) and _equal(x, kept)
+    flat = torch.zeros(200, dtype=torch.bfloat16, device="cuda")
+    for shift in (15, 33, 47):  # by 32 elements from head to head, 16 of them values: these share some
+        with pytest.raises(mp.MPError, match="overlaps"):
+            mp.mp_rope(*(flat[s:].as_strided((1, 3, 16), (96, 32, 1)) for s in (0, shift)), pos[:1], f)
+
+
 def test_one_page_beside_an_array_of_many(mp):
     """Keys in an array of their own, values in a page of a larger one whose stride differs."""
     import torch
