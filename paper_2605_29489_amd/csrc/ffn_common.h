@@ -1,5 +1,5 @@
-// Device helpers of the kernels that run a block's feed-forward part:
-// element access at any alignment, and the activations with their derivatives.
+// Device helpers of the kernels that run a block: element access at any
+// alignment, quotients, and the activations with their derivatives.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -21,6 +21,22 @@ struct Elem<MP_F32> {
 template <>
 struct Elem<MP_BF16> {
     using T = __bf16;
+};
+
+// Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and
+// m = ceil(2^(31+L) / d), n m / 2^(31+L) exceeds n / d by less than
+// n / 2^31 / d < 1 / d, so that their whole parts agree.
+struct Div {
+    uint32_t m = 0, shift = 0;
+    Div(uint32_t by = 1)
+    {
+        uint32_t L = 0;
+        while (((uint64_t)1 << L) < by)
+            ++L;
+        shift = 31 + L;
+        m = (uint32_t)((((uint64_t)1 << shift) + by - 1) / by);
+    }
+    __device__ inline uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
 };
 
 // ---------------------------------------------------------------- 16-byte access at element alignment

@@ -35,22 +35,6 @@ constexpr int kMinTiles = 4;  // tiles of a share at least
 constexpr int kShares = 256;  // one for each CU
 constexpr int kInStep = 2;    // tiles that the waves of a workgroup are apart at most
 
-// Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and
-// m = ceil(2^(31+L) / d), n m / 2^(31+L) exceeds n / d by less than
-// n / 2^31 / d < 1 / d, so that their whole parts agree.
-struct Div {
-    uint32_t m = 0, shift = 0;
-    Div(uint32_t by = 1)
-    {
-        uint32_t L = 0;
-        while (((uint64_t)1 << L) < by)
-            ++L;
-        shift = 31 + L;
-        m = (uint32_t)((((uint64_t)1 << shift) + by - 1) / by);
-    }
-    __device__ inline uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
-};
-
 struct AttendArgs {
     const char* k;
     const char* v;

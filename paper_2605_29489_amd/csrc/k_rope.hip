@@ -25,22 +25,6 @@ __device__ inline float2 turn_of(int64_t pos, double f, float amp)
     return make_float2(fmaf(-l, s, c) * amp, fmaf(l, c, s) * amp);
 }
 
-// Quotients of n < 2^31 by a divisor the host knows: with 2^(L-1) < d <= 2^L and
-// m = ceil(2^(31+L) / d), n m / 2^(31+L) exceeds n / d by less than
-// n / 2^31 / d < 1 / d, so that their whole parts agree.
-struct Div {
-    uint32_t m = 0, shift = 0, d = 1;
-    Div(uint32_t by = 1) : d(by)
-    {
-        uint32_t L = 0;
-        while (((uint64_t)1 << L) < by)
-            ++L;
-        shift = 31 + L;
-        m = (uint32_t)((((uint64_t)1 << shift) + by - 1) / by);
-    }
-    __device__ inline uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
-};
-
 // Outputs are written once and are more than the caches hold where it counts:
 // rotations of 16384 x 32 x 128 bf16 59.8 us with plain stores and 53.3 with
 // non-temporal ones, of 8192 x 40 x 128 39.0 and 28.6.  Non-temporal loads as
@@ -61,7 +45,7 @@ __device__ inline void st16n(void* p, uint4 c)
 struct TurnArgs {
     int64_t tokens;
     int tw;             // tokens of a workgroup
-    int dim, rot, per;  // items of a turned head
+    int dim, rot, per, copy;  // items of a turned head, and of a copied one
     uint32_t nx, nk, all;  // items of a token: x's, and keys', and all
     Div by_all, by_per, by_copy, by_page;
     const int64_t* pos;
@@ -120,7 +104,7 @@ __global__ __launch_bounds__(kThreads) void k_turn(TurnArgs a)
                 r -= a.nk;
                 kind = kValue;
                 h = a.by_copy.of(r);
-                j = (int)(r - h * a.by_copy.d);
+                j = (int)(r - h * a.copy);
                 p = static_cast<const T*>(a.v) + (t0 + t) * a.ldv + (int64_t)h * a.dim;
                 pair = false;
                 chunk = WHOLE || j < values;
@@ -244,14 +228,14 @@ hipError_t launch(TurnArgs& a, int dtype, bool interleaved, int64_t heads, int64
 {
     const int V = dtype == MP_F32 ? 4 : 8, half = a.rot / 2, pairs = interleaved ? V / 2 : V, rest = a.dim - a.rot;
     const bool whole = half % pairs == 0 && rest % V == 0;
-    const int copy = a.dim / V + a.dim % V;
+    a.copy = a.dim / V + a.dim % V;
     a.per = half / pairs + half % pairs + rest / V + rest % V;
     a.nx = (uint32_t)(heads * a.per);
     a.nk = a.nx + (uint32_t)(kv * a.per);
-    a.all = a.nk + (uint32_t)(kv * copy);
+    a.all = a.nk + (uint32_t)(kv * a.copy);
     a.by_all = Div(a.all);
     a.by_per = Div((uint32_t)a.per);
-    a.by_copy = Div((uint32_t)copy);
+    a.by_copy = Div((uint32_t)a.copy);
     // as many tokens as there are threads for
     const int64_t tw = std::max<int64_t>(1, std::min<int64_t>(kThreads / a.all, kMaxTurns / std::max(half, 1)));
     a.tw = (int)tw;
