@@ -17,8 +17,9 @@
 // so that ragged rows fill the chip evenly; a second kernel joins the parts of a
 // row.  bf16, 128 dims: 64 rows of 1 to 8192 keys of 8 heads (1.11 GB) 180 us, 172 of them
 // here (6.4 TB/s); the same rows of 4096 keys 173 us; one row of 131072 keys of
-// 4 heads (268 MB) 55 us, of which 40 at 6.7 TB/s, 2 before the first key arrives,
-// 3 joining the waves and 5 in the second kernel.
+// 4 heads (268 MB) 54 us, 6 of them in the second kernel; of the first one's 48 the
+// keys take 40 at 6.7 TB/s, 2 pass before the first of them arrives and 3 in joining
+// the waves.
 #include <algorithm>
 #include <type_traits>
 
@@ -31,9 +32,15 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kMinTiles = 4;  // tiles of a share at least
+// Tiles of a share at least.  One row of 4096 or 32768 keys (4 heads of 128 bf16
+// dims) 14.8 and 23.8 us, with 2 tiles the same, with 8 16.6 and 25.2; 8 rows of up
+// to 300 keys 27.7, with 8 32.2, with 2 14.6, as their shares then are enough for
+// equal parts of each row.
+constexpr int kMinTiles = 4;
 constexpr int kShares = 256;  // one for each CU
-constexpr int kInStep = 2;    // tiles that the waves of a workgroup are apart at most
+// Tiles that the waves of a workgroup are apart at most.  64 ragged rows of up to
+// 8192 keys / 256 of up to 700: 180 / 80 us; 1 apart 182 / 81, 4 180 / 81, 8 180 / 81.
+constexpr int kInStep = 2;
 
 struct AttendArgs {
     const char* k;
@@ -95,8 +102,9 @@ __device__ inline uint32_t work_of(const AttendArgs& a, int row)
 // of it, of `per` tiles from `at` on; it begins in `row`, whose first tile is at
 // row_at.
 // Where the tiles are few, a run is instead one of the equal parts of a row and
-// head set, so that no share holds two: 7 rows of up to 2000 fp32 keys 25.2 us
-// cut evenly, 21.5 so.
+// head set, so that no share holds two: 7 rows of up to 2000 fp32 keys 25.7 us
+// cut evenly, 21.3 so.  That is done up to a quarter of the shares in rows and head
+// sets: up to an eighth, 16 rows of up to 500 bf16 keys take 28.7 us for 15.9.
 struct Share {
     uint64_t at, end, row_at;
     uint32_t per, set_tiles;
@@ -265,10 +273,14 @@ __device__ inline uint4 ld16_few(const char* row, int d, int dim)
 }
 
 // N (8 or 16) bytes of a row of values.  A load instruction takes whole rows of
-// up to 256 bytes, which no other reads, so that they need not stay in the
-// caches; rows of keys are read in pieces of 64 bytes by several, and do.  64
-// rows of up to 8192 keys: 211 us without non-temporal loads, 193 with them for
-// the values, 192 for both; rows of 128 bytes: 86.6, 86.8 and 88.5 us.
+// up to 256 bytes, which, where a sequence has pages of its own and a head of the
+// cache one head tile, no other reads, so that they need not stay in the caches;
+// rows of keys are read in pieces of 64 bytes by several, and do.  64 rows of up
+// to 8192 keys (128 bf16 dims) 180 us, with plain loads 196; of 256 dims 183 and
+// 202; of 64 fp32 dims 186 and 204; one row of 131072 keys 55.4 and 59.5; rows of
+// 128 bytes 80 and 80.  Values that several read lose by it: three head tiles of a group of 48
+// of 256 dims 227 us, with plain loads 214; 8 rows of the same 65536 keys 99 and 88;
+// a prompt of 2048 tokens, a row each, 770 and 751.
 template <int N>
 __device__ inline uint4 ld_values(const char* p)
 {
@@ -718,7 +730,8 @@ pass:
                     sum[h] += p[h][e];
                 }
             }
-            // outputs
+            // Outputs.  In bf16 p enters as its rounding and the rounded remainder, two products, which keep 16 of its
+            // bits: 2^-16 of sum p |v| beside 2^-8 of the result when that is rounded.
             if constexpr (kBf16) {
                 uint4 hi[HT], lo[HT];
 #pragma unroll
@@ -1073,7 +1086,9 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a)
 
 // Four query heads a workgroup: a wave each where no head has more than kByWave
 // parts, else one after the other.  256 rows of 16 heads, few of them split: 8.9
-// us with a workgroup a head, 6.5 so.
+// us with a workgroup a head, 6.5 so.  With 4, 8, 16 and 32 parts a wave, the whole
+// attention of 64 rows of 32 heads and up to 8192 keys takes 185, 184, 180 and 180
+// us, of 24 such rows 84, 84, 84 and 80.
 constexpr int kByWave = 16;
 template <int DT, int LANES>
 __global__ __launch_bounds__(256) void k_join4(AttendArgs a)
@@ -1162,13 +1177,17 @@ Plan plan_of(const mp_kv_cache& c, const mp_kv_attend_shape& s)
     // a window may begin inside a tile, but a row has no more than its table has room for
     const bool slides = s.window > 0 && s.window < most;
     const int64_t tiles = slides ? std::min(tiles_in(s.window) + 1, tiles_in(most)) : tiles_in(most);
-    // a launch takes fewer than 2^32 threads along x
-    const int64_t threads = s.rows * p.head_tiles * 64 * waves_of(p.dp, p.ht, p.mode);
+    // Rows of few tiles are a workgroup each and head set, but for very many of them: 2^20 rows of up to 32 keys, 7
+    // heads of 64 dims, 29.1 ms in shares and 34.2 unsplit; of up to 64 keys, 8 heads of 128, 26.7 and 34.8.  (From
+    // 2^12 such rows on shares are the faster ones, 118 us for 136 and 115 for 137; at 1000 rows they are the same, at
+    // 64 16 us for 11; 20000 rows of 2 heads 565 for 528.)  The launch would hold either: rows <= 2^20 and rows *
+    // head_tiles <= rows * q_heads <= 2^23, and a set holds all head tiles or 4 of them at least, or 2 of 5, so that
+    // there are 3 * 2^20 workgroups of 1024 threads at most.
+    const int64_t waves = s.rows * p.head_tiles * waves_of(p.dp, p.ht, p.mode);
     // A share counts its tiles in 31 bits.  Tables with room for more have 2^13 rows and head sets or more, which
-    // fill the chip unsplit; and no 2^22, whose threads would be too many: rows * q_heads <= 2^23, and a set holds two
-    // head tiles or more where a row has that many.
+    // fill the chip unsplit.
     const int64_t all = s.rows * ((p.head_tiles + p.set_tiles - 1) / p.set_tiles) * tiles;
-    if (all < (int64_t)1 << 38 && (tiles > kMinTiles || threads >= (int64_t)1 << 32))
+    if (all < (int64_t)1 << 38 && (tiles > kMinTiles || waves >= (int64_t)1 << 26))
         p.shares = std::min<int64_t>(kShares, (s.rows * p.head_tiles * tiles + kMinTiles - 1) / kMinTiles);
     else if (p.one_if_few)
         p.set_tiles = 1;
@@ -1210,7 +1229,8 @@ void launch_type(const AttendArgs& a, const Plan& p, hipStream_t st)
         launch_tiles<DT, 256, 1>(a, grid, p.mode, st);
     if (p.shares) {
         // Few heads: their dims in slices of 32, so that more workgroups share the parts.  One row of 28 heads 55 us,
-        // by k_join4 85; 2048 heads 180 us, each in slices 189.
+        // by k_join4 85.  Rows of up to 8192 keys in slices / by k_join4, 128 dims: 256 heads 35 / 44, 512 58 / 63,
+        // 768 81 / 84, 1024 102 / 99, 1536 142 / 136; 64 dims: 384 heads 83 / 89, 640 125 / 125.
         const unsigned heads = (unsigned)(a.rows * a.heads * a.group);
         const unsigned fours = (unsigned)(a.rows * ((a.heads * a.group + 3) / 4));
         if (heads < 512)
